@@ -252,6 +252,87 @@ int tucker_attn_prepare_weights(tucker_attn_ctx *ctx, const tucker_attn_weights 
 int tucker_attn_release_weights(tucker_attn_ctx *ctx);
 
 /*
+ * Paged latent cache.  A serving program keeps the cached rows of all its sequences in one pool of pages per layer and names the
+ * pages of every sequence in a table, so that sequences grow without being moved and share the pages of a common beginning.
+ */
+
+/* One layer's pool; plain host data, device pointers caller-owned. */
+typedef struct {
+  void *K;                /* device [n_pages][page_size][r3]   rotated keys (with shared_kv: the unrotated latent)        */
+  void *V;                /* device [n_pages][page_size][rt3]  values; NULL with shared_kv                                */
+  int64_t k_stride;       /* elements from one page to the next (several layers' or both pools in one allocation); 0:    */
+  int64_t v_stride;       /* pages lie one behind the other.  At least page_size * r3 (rt3), a multiple of 16 bytes      */
+  int32_t n_pages, page_size;   /* page_size: any number of rows from 1 on                                               */
+} tucker_attn_pages;
+
+/* The sequences of one step: sequence b brings the tokens q_start[b] .. q_start[b+1]-1 of the step's T token rows (none: its
+ * table is not looked at) and has kv_len[b] cached rows, its new tokens included and last: new token j of q sits at position
+ * kv_len[b] - q + j.  Row n of a sequence is row n % page_size of page page_table[b][n / page_size].
+ * The three arrays live on the device, so a captured graph serves steps whose lengths and pages change; the host knows bounds.
+ * Values outside what is stated here lead to wrong results, never out of a buffer: counts and lengths are cut to the bounds, a
+ * page number outside the pool is read as page 0 and not written. */
+typedef struct {
+  const int32_t *q_start;     /* device [B+1]            q_start[0] = 0, not decreasing, q_start[B] <= T: the token rows behind */
+                              /*                         it are padding, neither read nor written                        */
+  const int32_t *kv_len;      /* device [B]              at least the sequence's number of new tokens                     */
+  const int32_t *page_table;  /* device [B][max_pages]   entries behind a sequence's last page are not looked at          */
+  int32_t B, T;
+  int32_t max_pages;          /* entries of a table row                                                                   */
+  int32_t max_new, max_len;   /* no sequence brings more new tokens, or has more cached rows; max_len <= max_pages *      */
+                              /* page_size, and <= max_positions with latent RoPE                                         */
+} tucker_attn_batch;
+
+/*
+ * The new tokens' latent rows go into their pages, rotated on the way (Sections "KV Caching" and "Rotary Position Embedding"):
+ * key row t to its token's position (unless the latent is shared: unrotated), value row t as it is; and the per-head queries of
+ * the tokens are rotated by the same angles.
+ *   K        device [T] rows of r3 elements, ldk apart      in: key latents X U3, unrotated (shared_kv: the latent)
+ *   V        device [T] rows of rt3 elements, ldv apart     in: value latents X U~3; NULL with shared_kv
+ *   Q, Qrot  device [T, n_heads, r3]                        in, out (both or neither; may be the same array): per-head queries
+ *   rotate   1; 0: K rows are stored as they come (rows that tucker_attn_forward left in a contiguous cache are rotated
+ *            already), and Q must be NULL.  Without latent RoPE nothing is rotated
+ * A token before its sequence's first row (kv_len too small) is not stored.  Two tokens that name the same row are a race.
+ * Any alignment of K, V, Q, Qrot and of ldk, ldv; rows that start on 16 bytes are read and written whole.
+ * UNSUPPORTED_SHAPE: pool rows that are no multiple of 16 bytes; T * n_heads of 2^31 and more.
+ */
+int tucker_attn_append_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
+                             const void *K, int64_t ldk, const void *V, int64_t ldv, const void *Q, void *Qrot,
+                             int32_t rotate, void *hip_stream);
+
+/* Bytes of device workspace the two calls below need for a batch of these bounds (prefix_len 0: the first one); 0 if an argument
+ * is invalid.  The arrays of the batch are not looked at. */
+size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tucker_attn_batch *batch, int32_t prefix_len);
+
+/*
+ * Attention of the new tokens over the pages of their sequences (Section "Flash Attention" with one key-value row for all heads):
+ *   S[t,i,n] = <Q[t,i], K row n of t's sequence> / sqrt(d_head),  lse[t,i] = log sum_n exp S[t,i,n],
+ *   O[t,i] = sum_n exp(S[t,i,n] - lse[t,i]) V row n
+ * over the rows n up to t's own position (all kv_len rows if the context is not causal).  With shared_kv the key is the latent
+ * row rotated to n and the value the row itself.  A token that sees no row has O = 0 and lse = -infinity.  What rows that a token
+ * does not see hold (Inf and NaN included) does not reach it.
+ *   Q    device [T, n_heads, r3]   in: per-head queries, rotated (Qrot of tucker_attn_append_paged)
+ *   O    device [T, n_heads, rt3]  out, storage type
+ *   lse  device [T, n_heads] fp32  out, natural logarithm; may be NULL
+ * One new token per sequence (decode), a few (proposed tokens) or many (pieces of a prompt).  Q and O start on 16 bytes.
+ * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; T * n_heads of 2^31 and more.
+ */
+int tucker_attn_attend_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
+                             const void *Q, void *O, float *lse, void *workspace, size_t workspace_bytes,
+                             void *hip_stream);
+
+/*
+ * tucker_attn_attend_paged for a batch whose sequences begin with the same prefix_len rows, held once in pages of their own:
+ * row n < prefix_len of every sequence is row n % page_size of page prefix_table[n / page_size] (the first prefix_len / page_size
+ * entries of the sequences' tables are not looked at; a prefix that ends inside a page has its last rows in both).  These rows
+ * are read, and multiplied with the queries of all tokens, once.  Every new token lies behind the prefix.
+ *   prefix_table   device [ceil(prefix_len / page_size)]; may be NULL if prefix_len is 0
+ * The other arguments, the results and the refusals are those of tucker_attn_attend_paged.
+ */
+int tucker_attn_attend_prefix(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
+                              const int32_t *prefix_table, int32_t prefix_len, const void *Q, void *O, float *lse,
+                              void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Optional per-kernel timing for benchmarks.  While enabled, forward/backward/decode bracket every
  * kernel they launch with HIP events recorded on the caller's stream; tucker_attn_profile_read
  * synchronises those events and returns, for the LAST call, the kernel count and for each

@@ -23,6 +23,7 @@ EXPORTED = [
     "tucker_attn_decode_workspace_bytes", "tucker_attn_forward", "tucker_attn_decode", "tucker_attn_decode_static",
     "tucker_attn_backward_workspace_bytes", "tucker_attn_backward",
     "tucker_attn_prepared_weights_bytes", "tucker_attn_prepare_weights", "tucker_attn_release_weights",
+    "tucker_attn_append_paged", "tucker_attn_attend_workspace_bytes", "tucker_attn_attend_paged", "tucker_attn_attend_prefix",
     "tucker_attn_profile_enable", "tucker_attn_profile_read", "tucker_attn_measure_mfma_ceiling",
     "tucker_attn_status_string",
 ]
@@ -54,6 +55,46 @@ GRAD_KEYS = ("dC", "dU1", "dU2", "dU3", "dCt", "dUt1", "dUt2", "dUt3")
 
 class tucker_attn_grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in GRAD_KEYS]
+
+
+class tucker_attn_pages(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+    @classmethod
+    def of(cls, K, V=None) -> "tucker_attn_pages":
+        """One layer's pool.  K: device tensor [pages, rows of a page, r3], V: [pages, rows of a page, rt3] (None with a shared
+        key-value latent); pages may lie apart (any stride of the first dimension), rows may not.  The structure holds the tensors."""
+        for t in (K, V):
+            if t is not None and (t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]):
+                raise TuckerAttnError("a pool is [pages, rows of a page, r] with contiguous pages")
+        if V is not None and (V.shape[:2] != K.shape[:2] or V.dtype != K.dtype or V.device != K.device):
+            raise TuckerAttnError("key and value pools have the same pages, storage type and device")
+        s = cls(K.data_ptr(), _ptr(V), K.stride(0), 0 if V is None else V.stride(0), K.shape[0], K.shape[1])
+        s.tensors = (K, V)
+        s.r3, s.rt3, s.dtype = K.shape[2], K.shape[2] if V is None else V.shape[2], K.dtype
+        return s
+
+
+class tucker_attn_batch(C.Structure):
+    _fields_ = [("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("B", C.c_int32), ("T", C.c_int32),
+                ("max_pages", C.c_int32), ("max_new", C.c_int32), ("max_len", C.c_int32)]
+
+    @classmethod
+    def of(cls, q_start, kv_len, page_table, *, tokens: int, max_new: int, max_len: int) -> "tucker_attn_batch":
+        """The sequences of a step, for all layers.  q_start [B+1], kv_len [B], page_table [B, max_pages]: contiguous int32 device
+        tensors, whose values may change between calls; tokens, max_new, max_len: rows of the token arrays and the bounds.
+        The structure holds the tensors."""
+        B = int(kv_len.shape[0])
+        if tuple(q_start.shape) != (B + 1,) or page_table.dim() != 2 or page_table.shape[0] != B:
+            raise TuckerAttnError("q_start is [B + 1], kv_len [B], page_table [B, max_pages]")
+        for t in (q_start, kv_len, page_table):
+            if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+                raise TuckerAttnError("the arrays of a batch are contiguous int32 tensors")
+        s = cls(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), B, int(tokens), int(page_table.shape[1]),
+                int(max_new), int(max_len))
+        s.tensors = (q_start, kv_len, page_table)
+        return s
 
 
 WEIGHT_KEYS = ("C", "U1", "U2", "U3", "Ct", "Ut1", "Ut2", "Ut3")
@@ -118,6 +159,18 @@ def load_library() -> C.CDLL:
     lib.tucker_attn_prepare_weights.restype = C.c_int
     lib.tucker_attn_release_weights.argtypes = [ctx_p]
     lib.tucker_attn_release_weights.restype = C.c_int
+    pages_p, batch_p = C.POINTER(tucker_attn_pages), C.POINTER(tucker_attn_batch)
+    lib.tucker_attn_append_paged.argtypes = [ctx_p, pages_p, batch_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                             C.c_void_p, C.c_int32, C.c_void_p]
+    lib.tucker_attn_append_paged.restype = C.c_int
+    lib.tucker_attn_attend_workspace_bytes.argtypes = [ctx_p, batch_p, C.c_int32]
+    lib.tucker_attn_attend_workspace_bytes.restype = C.c_size_t
+    lib.tucker_attn_attend_paged.argtypes = [ctx_p, pages_p, batch_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                             C.c_void_p]
+    lib.tucker_attn_attend_paged.restype = C.c_int
+    lib.tucker_attn_attend_prefix.argtypes = [ctx_p, pages_p, batch_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                              C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tucker_attn_attend_prefix.restype = C.c_int
     lib.tucker_attn_profile_enable.argtypes = [ctx_p, C.c_int32]
     lib.tucker_attn_profile_enable.restype = C.c_int
     lib.tucker_attn_profile_read.argtypes = [ctx_p, C.POINTER(C.c_char_p), C.POINTER(C.c_float), C.c_int32]
@@ -287,6 +340,73 @@ def tucker_attn_prepare_weights(ctx: int, weights: Dict, prepared, stream=None, 
 
 def tucker_attn_release_weights(ctx: int) -> None:
     _check(load_library().tucker_attn_release_weights(ctx), "tucker_attn_release_weights")
+
+
+# ---- paged latent cache ---------------------------------------------------------------------------------------
+
+def _rows(t, batch: tucker_attn_batch, width: int, pages: tucker_attn_pages, name: str) -> None:
+    if t.shape[0] != batch.T or t.shape[-1] != width or t.dtype != pages.dtype:
+        raise TuckerAttnError(f"{name}: {tuple(t.shape)} {t.dtype} where {batch.T} token rows of {width} {pages.dtype} are expected")
+
+
+def tucker_attn_append_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, K, V=None, Q=None, Qrot=None,
+                             rotate: bool = True, stream=None, check: bool = True) -> int:
+    """K: [T, r3], V: [T, rt3] (None with a shared latent), rows may lie apart (columns of a wider array); Q, Qrot: contiguous
+    [T, n_heads, r3], or neither."""
+    _rows(K, batch, pages.r3, pages, "K")
+    if V is not None:
+        _rows(V, batch, pages.rt3, pages, "V")
+    for t in (Q, Qrot):
+        if t is not None:
+            _rows(t, batch, pages.r3, pages, "Q, Qrot")
+            if not t.is_contiguous():
+                raise TuckerAttnError("Q and Qrot are contiguous")
+    if K.stride(1) != 1 or (V is not None and V.stride(1) != 1):
+        raise TuckerAttnError("the channels of a K or V row are contiguous")
+    st = load_library().tucker_attn_append_paged(ctx, C.byref(pages), C.byref(batch), K.data_ptr(), K.stride(0), _ptr(V),
+                                                 0 if V is None else V.stride(0), _ptr(Q), _ptr(Qrot), int(bool(rotate)),
+                                                 _stream_ptr(stream))
+    if check:
+        _check(st, "tucker_attn_append_paged")
+    return st
+
+
+def tucker_attn_attend_workspace_bytes(ctx: int, batch: tucker_attn_batch, prefix_len: int = 0) -> int:
+    return int(load_library().tucker_attn_attend_workspace_bytes(ctx, C.byref(batch), prefix_len))
+
+
+def _attend_rows(pages, batch, Q, O, lse) -> None:
+    _rows(Q, batch, pages.r3, pages, "Q")
+    _rows(O, batch, pages.rt3, pages, "O")
+    if not (Q.is_contiguous() and O.is_contiguous() and (lse is None or lse.is_contiguous())):
+        raise TuckerAttnError("Q, O and lse are contiguous")
+
+
+def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, Q, O, lse=None, workspace=None,
+                             stream=None, check: bool = True) -> int:
+    """Q: [T, n_heads, r3], O: [T, n_heads, rt3], lse: fp32 [T, n_heads] or None; workspace: device uint8 tensor of at least
+    tucker_attn_attend_workspace_bytes bytes."""
+    _attend_rows(pages, batch, Q, O, lse)
+    st = load_library().tucker_attn_attend_paged(ctx, C.byref(pages), C.byref(batch), Q.data_ptr(), O.data_ptr(), _ptr(lse),
+                                                 _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                                 _stream_ptr(stream))
+    if check:
+        _check(st, "tucker_attn_attend_paged")
+    return st
+
+
+def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, prefix_table, prefix_len: int, Q, O,
+                              lse=None, workspace=None, stream=None, check: bool = True) -> int:
+    """tucker_attn_attend_paged behind a common prefix; prefix_table: int32 device tensor with the pages of its rows."""
+    _attend_rows(pages, batch, Q, O, lse)
+    if prefix_len > 0 and (str(prefix_table.dtype) != "torch.int32" or prefix_table.numel() * pages.page_size < prefix_len):
+        raise TuckerAttnError("prefix_table: int32, a page for every page_size rows of the prefix")
+    st = load_library().tucker_attn_attend_prefix(ctx, C.byref(pages), C.byref(batch), _ptr(prefix_table), int(prefix_len),
+                                                  Q.data_ptr(), O.data_ptr(), _ptr(lse), _ptr(workspace),
+                                                  0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if check:
+        _check(st, "tucker_attn_attend_prefix")
+    return st
 
 
 def tucker_attn_profile_enable(ctx: int, on: bool) -> None:

@@ -1,0 +1,139 @@
+// The paged latent cache: arguments and launchers of the append and attention kernels, and the device functions they share
+// (sequence bounds, page lookup, output rows).
+#pragma once
+#include "common.h"
+#include "params.h"
+
+namespace ta {
+
+// n / d for 0 <= n < 2^31 by one high product: mul = ceil(2^(31+shift) / d), shift = ceil(log2 d)
+struct Divisor {
+  uint32_t mul;
+  int shift;
+};
+inline Divisor divisor(int d) {
+  int s = 0;
+  while ((1l << s) < d) ++s;
+  return {(uint32_t)(((1ul << (31 + s)) + d - 1) / d), s};
+}
+
+struct PagedArgs {
+  // pool: page j of the keys starts k_stride * j elements behind K, its rows r3 wide; values alike (null: shared latent)
+  const void *K, *V;
+  long k_stride, v_stride;
+  int n_pages, page_size;
+  Divisor ps;
+  // batch: device arrays as the header describes them, and the bounds that keep every access inside the buffers
+  const int *q_start, *kv_len, *table;
+  int B, T, max_pages, max_new, max_len;
+  const int* prefix_table;      // pages of rows 0 .. prefix-1 of every sequence
+  int prefix;                   // 0: none
+  // queries [T][nH] rows of q_row elements, outputs [T][nH] rows of o_row elements, log-sum-exp [T][nH] (nullable)
+  const void* Q;
+  void* O;
+  float* lse;
+  int q_row, o_row, o_acc;      // o_acc: output channels at their acc-order positions, all D of them
+  int nH, r3, rt3, D;
+  Divisor heads;
+  float scale;                  // of a score, times log2(e)
+  int causal, shared_kv;
+  const float4* rope;           // [D/4][rope_ld] as in GemmArgs, or null; read for a shared latent only
+  int rope_ld;
+  // partial results of a row (un-normalised output in fp32; running maximum in the base-2 domain and sum)
+  float* part_o;                // [parts][T * nH][D]
+  float2* part_ml;              // [parts][T * nH]
+  int prefix_parts;             // parts 0 .. prefix_parts-1: the prefix
+  int own_parts;                // then those of the sequence's own rows; 0: written to O directly
+};
+
+// Latent rows into their pages, keys (and the per-head queries, if given) rotated to the tokens' positions
+struct PagedAppendArgs {
+  void *K, *V;                  // pools as above
+  long k_stride, v_stride;
+  int n_pages, page_size;
+  Divisor ps;
+  const int *q_start, *kv_len, *table;
+  int B, T, max_pages, max_new, max_len;
+  const void *Kin, *Vin, *Qin;  // rows of ldk, ldv elements; [T][nH] rows of q_row elements
+  void* Qout;
+  long ldk, ldv;
+  int q_row, nH, r3, rt3;
+  int rotate_k;                 // 0: key rows are stored as they come
+  const float4* rope;           // null: nothing is rotated
+  int rope_ld;
+};
+
+int paged_rows_blocks(const PagedArgs& a, int rows);   // row blocks of `rows` rows that a batch can have
+hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s);
+hipError_t launch_paged_rows(int dtype, const PagedArgs& a, bool prefix_pass, hipStream_t s);
+hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s);
+
+// ---- device -----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int divide(int n, Divisor d) { return (int)(__umulhi((uint32_t)n * 2u, d.mul) >> d.shift); }
+
+// Sequence b of a batch.  What the arrays hold is bounded here, so that no value in them leads outside a buffer.
+struct PagedSeq {
+  int q0, nq;                   // its new tokens
+  int len;                      // its cached rows
+};
+template <typename A> __device__ __forceinline__ PagedSeq paged_seq(const A& p, int b) {
+  PagedSeq s;
+  const int q1 = min(max(p.q_start[b + 1], 0), p.T);
+  s.q0 = min(max(p.q_start[b], 0), p.T);
+  s.nq = min(max(q1 - s.q0, 0), p.max_new);
+  s.len = min(max(p.kv_len[b], 0), p.max_len);
+  return s;
+}
+
+// Page of row n (n / page size = i) by a table of `entries` entries; a number that is no page of the pool reads page 0
+__device__ __forceinline__ int paged_page(const int* table, int i, int n_pages) {
+  const int page = table[i];
+  return (uint32_t)page < (uint32_t)n_pages ? page : 0;
+}
+
+// Which sequence item `target` belongs to when every sequence has items(b) of them, one behind the other: its number (-1: behind
+// the last), the item's index in it, and the number of all items.  All 256 threads call; `sh` holds 8 words.
+template <class F>
+__device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh, int& index, int& total) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int per = (B + 255) / 256, first = tid * per, last = min(B, first + per);
+  int mine = 0;
+  for (int b = first; b < last; ++b) mine += items(b);
+  int x = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == kWave - 1) sh[wave] = x;
+  if (tid == 0) sh[4] = -1;
+  __syncthreads();
+  total = sh[0] + sh[1] + sh[2] + sh[3];
+  int before = x - mine;
+  for (int w = 0; w < wave; ++w) before += sh[w];
+  if (target >= before && target < before + mine) {
+    int b = first;
+    for (int n; target >= before + (n = items(b)); ++b) before += n;
+    sh[4] = b;
+    sh[5] = target - before;
+  }
+  __syncthreads();
+  index = sh[5];
+  const int found = sh[4];
+  __syncthreads();
+  return found;
+}
+
+// four output channels c .. c+3 of one row
+template <typename T>
+__device__ __forceinline__ void paged_store4(const PagedArgs& p, long row, int c, f32x4 v) {
+  T* o = static_cast<T*>(p.O) + row * p.o_row;
+  if (p.o_acc) {
+    if (c >= p.rt3) v = f32x4{0.f, 0.f, 0.f, 0.f};
+    store4(o + (c & ~31) + acc_pos(c & 31), v[0], v[1], v[2], v[3]);
+  }
+  else if (c < p.rt3) store4(o + c, v[0], v[1], v[2], v[3]);
+}
+constexpr float kLn2 = 0.69314718055994531f;
+
+}  // namespace ta

@@ -1,0 +1,151 @@
+// Host side of the paged latent cache: argument checks, the split of a call's work, launches.
+#include "context.h"
+#include "paged.h"
+
+using namespace ta;
+
+namespace {
+
+constexpr long kMaxRows = 1l << 31;   // (token, head) rows of a call
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int check_batch(const tucker_attn_ctx* c, const tucker_attn_batch* b) {
+  if (!c || !b || b->B < 1 || b->T < 1 || b->max_pages < 1 || b->max_new < 1 || b->max_len < 1) return TUCKER_ATTN_INVALID_ARG;
+  const tucker_attn_config& f = c->cfg;
+  if (f.use_rope && b->max_len > f.max_positions) return TUCKER_ATTN_INVALID_ARG;
+  if ((long)b->T * f.n_heads >= kMaxRows) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
+  if ((f.r3 * c->es) % 16 != 0 || (f.rt3 * c->es) % 16 != 0) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
+  return TUCKER_ATTN_OK;
+}
+
+int check_pool(const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucker_attn_batch* b) {
+  if (!p || !p->K || p->n_pages < 1 || p->page_size < 1) return TUCKER_ATTN_INVALID_ARG;
+  const tucker_attn_config& f = c->cfg;
+  if (f.shared_kv ? p->V != nullptr : p->V == nullptr) return TUCKER_ATTN_INVALID_ARG;
+  if (!aligned16(p->K) || !aligned16(p->V)) return TUCKER_ATTN_INVALID_ARG;
+  auto stride_ok = [&](int64_t s, int r) { return s == 0 || (s >= (int64_t)p->page_size * r && (s * c->es) % 16 == 0); };
+  if (!stride_ok(p->k_stride, f.r3) || (!f.shared_kv && !stride_ok(p->v_stride, f.rt3))) return TUCKER_ATTN_INVALID_ARG;
+  if (!b->q_start || !b->kv_len || !b->page_table) return TUCKER_ATTN_INVALID_ARG;
+  if (b->max_len > (long)b->max_pages * p->page_size) return TUCKER_ATTN_INVALID_ARG;
+  return TUCKER_ATTN_OK;
+}
+
+template <typename A> void fill(A& a, const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucker_attn_batch* b) {
+  const tucker_attn_config& f = c->cfg;
+  a.K = p->K; a.V = p->V;
+  a.k_stride = p->k_stride ? p->k_stride : (long)p->page_size * f.r3;
+  a.v_stride = p->v_stride ? p->v_stride : (long)p->page_size * f.rt3;
+  a.n_pages = p->n_pages; a.page_size = p->page_size; a.ps = divisor(p->page_size);
+  a.q_start = b->q_start; a.kv_len = b->kv_len; a.table = b->page_table;
+  a.B = b->B; a.T = b->T; a.max_pages = b->max_pages; a.max_new = b->max_new; a.max_len = b->max_len;
+  a.nH = f.n_heads; a.r3 = f.r3; a.rt3 = f.rt3;
+  a.rope = c->rope; a.rope_ld = f.max_positions;
+}
+
+// Parts that the keys of a product of `blocks` row blocks are dealt to: two workgroups for every compute unit, and no part of
+// fewer than 128 keys
+int key_parts(const tucker_attn_ctx* c, long blocks, int keys) {
+  const long most = (keys + 127) / 128, want = 2l * c->n_cus / (blocks < 1 ? 1 : blocks);
+  return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+}
+
+// What of a call's arguments depends on its bounds alone: parts, and with them the workspace
+struct AttendWs {
+  size_t bytes;
+};
+AttendWs plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, void* ws, PagedArgs& a) {
+  const tucker_attn_config& f = c->cfg;
+  a.B = b->B; a.T = b->T; a.nH = f.n_heads; a.D = c->D; a.prefix = prefix;
+  const long rows = (long)b->T * f.n_heads;
+  a.prefix_parts = prefix > 0 ? key_parts(c, (rows + 31) / 32, prefix) : 0;
+  a.own_parts = key_parts(c, paged_rows_blocks(a, 32), b->max_len - prefix);
+  if (a.own_parts == 1 && prefix == 0) a.own_parts = 0;
+  const size_t parts = a.prefix_parts + a.own_parts;
+  Carver cv{static_cast<char*>(ws), 0};
+  a.part_o = cv.take<float>(parts * rows * c->D * 4);
+  a.part_ml = cv.take<float2>(parts * rows * 8);
+  return {cv.off};
+}
+
+int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const int32_t* prefix_table,
+           int32_t prefix, const void* Q, void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int st = check_batch(c, batch)) return st;
+  if (int st = check_pool(c, pages, batch)) return st;
+  if (!Q || !O || !aligned16(Q) || !aligned16(O) || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return TUCKER_ATTN_INVALID_ARG;
+  if (prefix < 0 || prefix > batch->max_len || (prefix > 0 && !prefix_table)) return TUCKER_ATTN_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return TUCKER_ATTN_INVALID_ARG;
+  const tucker_attn_config& f = c->cfg;
+  PagedArgs a;
+  std::memset(&a, 0, sizeof(a));
+  fill(a, c, pages, batch);
+  a.prefix_table = prefix_table;
+  a.Q = Q; a.O = O; a.lse = lse; a.q_row = f.r3; a.o_row = f.rt3;
+  a.heads = divisor(f.n_heads); a.scale = c->qscale; a.causal = f.causal; a.shared_kv = f.shared_kv;
+  const AttendWs ws = plan(c, batch, prefix, workspace, a);
+  if (ws.bytes > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
+  if (workspace_bytes < ws.bytes) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
+
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  Recorder rec{c, s, c->profile != 0};
+  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (prefix > 0) {
+    if (launch_paged_rows(f.dtype, a, true, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+    (void)rec.after("prefix_attention");
+  }
+  if (launch_paged_rows(f.dtype, a, false, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("paged_attention");
+  if (a.prefix_parts + a.own_parts > 0) {
+    if (launch_paged_merge(f.dtype, a, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+    (void)rec.after("paged_merge");
+  }
+  return TUCKER_ATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tucker_attn_append_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const void* K,
+                             int64_t ldk, const void* V, int64_t ldv, const void* Q, void* Qrot, int32_t rotate,
+                             void* hip_stream) {
+  if (int st = check_batch(c, batch)) return st;
+  if (int st = check_pool(c, pages, batch)) return st;
+  const tucker_attn_config& f = c->cfg;
+  if (!K || (f.shared_kv ? V != nullptr : V == nullptr) || (Q == nullptr) != (Qrot == nullptr)) return TUCKER_ATTN_INVALID_ARG;
+  if (rotate != 0 && rotate != 1) return TUCKER_ATTN_INVALID_ARG;
+  if (!rotate && Q) return TUCKER_ATTN_INVALID_ARG;
+  if (ldk < f.r3 || (V && ldv < f.rt3)) return TUCKER_ATTN_INVALID_ARG;
+  for (const void* p : {K, V, Q, static_cast<const void*>(Qrot)})
+    if (reinterpret_cast<uintptr_t>(p) % c->es != 0) return TUCKER_ATTN_INVALID_ARG;
+  PagedAppendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  fill(a, c, pages, batch);
+  a.Kin = K; a.ldk = ldk; a.Vin = V; a.ldv = ldv; a.Qin = Q; a.Qout = Qrot; a.q_row = f.r3;
+  a.rotate_k = rotate && !f.shared_kv;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  Recorder rec{c, s, c->profile != 0};
+  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (launch_paged_append(f.dtype, a, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("paged_append");
+  return TUCKER_ATTN_OK;
+}
+
+size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx* c, const tucker_attn_batch* batch, int32_t prefix_len) {
+  if (check_batch(c, batch) != TUCKER_ATTN_OK || prefix_len < 0 || prefix_len > batch->max_len) return 0;
+  PagedArgs a;
+  return plan(c, batch, prefix_len, nullptr, a).bytes;
+}
+
+int tucker_attn_attend_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const void* Q,
+                             void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend(c, pages, batch, nullptr, 0, Q, O, lse, workspace, workspace_bytes, hip_stream);
+}
+
+int tucker_attn_attend_prefix(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch,
+                              const int32_t* prefix_table, int32_t prefix_len, const void* Q, void* O, float* lse,
+                              void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend(c, pages, batch, prefix_table, prefix_len, Q, O, lse, workspace, workspace_bytes, hip_stream);
+}
+
+}  // extern "C"
