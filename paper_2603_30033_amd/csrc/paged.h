@@ -44,7 +44,13 @@ struct PagedArgs {
   float2* part_ml;              // [parts][T * nH]
   int prefix_parts;             // parts 0 .. prefix_parts-1: the prefix
   int own_parts;                // then those of the sequence's own rows; 0: written to O directly
+  // few rows a sequence (paged_stream): 32-row blocks of a sequence, workgroups that share all sequences' keys (0: one for every
+  // sequence), and partial results of sequences that several share, [2 * stream_wgs][hb * 32] rows
+  int hb, stream_wgs;
+  float* stream_o;
+  float2* stream_ml;
 };
+constexpr int kStreamUnit = 128, kStreamLeast = 2;   // keys of a unit of that kernel's work, least units of a workgroup
 
 // Latent rows into their pages, keys (and the per-head queries, if given) rotated to the tokens' positions
 struct PagedAppendArgs {
@@ -66,6 +72,8 @@ struct PagedAppendArgs {
 int paged_rows_blocks(const PagedArgs& a, int rows);   // row blocks of `rows` rows that a batch can have
 hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s);
 hipError_t launch_paged_rows(int dtype, const PagedArgs& a, bool prefix_pass, hipStream_t s);
+hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16
+hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s);     // of its partial results, and the prefix's
 hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s);
 
 // ---- device -----------------------------------------------------------------------------------------------------

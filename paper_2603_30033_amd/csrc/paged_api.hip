@@ -50,22 +50,32 @@ int key_parts(const tucker_attn_ctx* c, long blocks, int keys) {
   return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
-// What of a call's arguments depends on its bounds alone: parts, and with them the workspace
-struct AttendWs {
-  size_t bytes;
-};
-AttendWs plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, void* ws, PagedArgs& a) {
+// Longest keys that one workgroup takes alone rather than several and a second launch that joins their results
+constexpr int kStreamWhole = 512;
+
+// What of a call depends on its bounds alone: which kernels, the parts of their work, the workspace.  Returns its bytes.
+size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, void* ws, PagedArgs& a) {
   const tucker_attn_config& f = c->cfg;
   a.B = b->B; a.T = b->T; a.nH = f.n_heads; a.D = c->D; a.prefix = prefix;
-  const long rows = (long)b->T * f.n_heads;
+  const long rows = (long)b->T * f.n_heads, most = (long)b->max_new * f.n_heads;
+  const int keys = b->max_len - prefix;
+  a.hb = f.dtype != TUCKER_ATTN_BF16 ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
   a.prefix_parts = prefix > 0 ? key_parts(c, (rows + 31) / 32, prefix) : 0;
-  a.own_parts = key_parts(c, paged_rows_blocks(a, 32), b->max_len - prefix);
-  if (a.own_parts == 1 && prefix == 0) a.own_parts = 0;
-  const size_t parts = a.prefix_parts + a.own_parts;
+  a.stream_wgs = 0;
+  if (a.hb > 0) {
+    a.own_parts = prefix > 0 ? 1 : 0;                             // sequences that one workgroup does alone
+    if (keys > kStreamWhole) a.stream_wgs = c->n_cus;
+  } else {
+    a.own_parts = key_parts(c, paged_rows_blocks(a, 32), keys);
+    if (a.own_parts == 1 && prefix == 0) a.own_parts = 0;
+  }
+  const size_t parts = a.prefix_parts + a.own_parts, shared = 2ul * a.stream_wgs * a.hb * 32;
   Carver cv{static_cast<char*>(ws), 0};
   a.part_o = cv.take<float>(parts * rows * c->D * 4);
   a.part_ml = cv.take<float2>(parts * rows * 8);
-  return {cv.off};
+  a.stream_o = cv.take<float>(shared * c->D * 4);
+  a.stream_ml = cv.take<float2>(shared * 8);
+  return cv.off;
 }
 
 int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const int32_t* prefix_table,
@@ -82,9 +92,9 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
   a.prefix_table = prefix_table;
   a.Q = Q; a.O = O; a.lse = lse; a.q_row = f.r3; a.o_row = f.rt3;
   a.heads = divisor(f.n_heads); a.scale = c->qscale; a.causal = f.causal; a.shared_kv = f.shared_kv;
-  const AttendWs ws = plan(c, batch, prefix, workspace, a);
-  if (ws.bytes > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
-  if (workspace_bytes < ws.bytes) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
+  const size_t need = plan(c, batch, prefix, workspace, a);
+  if (need > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
+  if (workspace_bytes < need) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
 
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
@@ -93,10 +103,10 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
     if (launch_paged_rows(f.dtype, a, true, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("prefix_attention");
   }
-  if (launch_paged_rows(f.dtype, a, false, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if ((a.hb > 0 ? launch_paged_stream(a, s) : launch_paged_rows(f.dtype, a, false, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("paged_attention");
-  if (a.prefix_parts + a.own_parts > 0) {
-    if (launch_paged_merge(f.dtype, a, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (a.prefix_parts + a.own_parts + a.stream_wgs > 0) {
+    if ((a.hb > 0 ? launch_paged_join(a, s) : launch_paged_merge(f.dtype, a, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("paged_merge");
   }
   return TUCKER_ATTN_OK;
@@ -134,7 +144,7 @@ int tucker_attn_append_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages,
 size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx* c, const tucker_attn_batch* batch, int32_t prefix_len) {
   if (check_batch(c, batch) != TUCKER_ATTN_OK || prefix_len < 0 || prefix_len > batch->max_len) return 0;
   PagedArgs a;
-  return plan(c, batch, prefix_len, nullptr, a).bytes;
+  return plan(c, batch, prefix_len, nullptr, a);
 }
 
 int tucker_attn_attend_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const void* Q,

@@ -5,108 +5,9 @@
 //
 //   paged_rows   32 rows a workgroup, its four waves taking every fourth block of 32 keys straight from the pages
 //   paged_merge  joins the partial results of a row: sum_i 2^(m_i - m) (l_i, O_i), m = max m_i
-#include "paged.h"
+#include "paged_block.h"
 
 namespace ta {
-
-// 16 channels c0 .. of a row of r channels (whole 16-byte chunks), zeros behind them
-template <typename T> __device__ __forceinline__ Frag<T> load_frag_upto(const T* row, int c0, int r) {
-  constexpr int CE = 16 / (int)sizeof(T), NC = 16 / CE;
-  Frag<T> f = zero_frag<T>();
-#pragma unroll
-  for (int i = 0; i < NC; ++i)
-    if (c0 + i * CE < r) f.v[i] = *reinterpret_cast<const decltype(f.v[0] + f.v[0])*>(row + c0 + i * CE);
-  return f;
-}
-
-// the fragment's 8 channel pairs turned by the table entries of their 4 quads
-__device__ __forceinline__ void turn_frag(Frag<bf16>& f, const f32x4 (&cs)[4]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    u32x4 raw = __builtin_bit_cast(u32x4, f.v[i]);
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const float c = cs[2 * i + d / 2][2 * (d % 2)], s = cs[2 * i + d / 2][2 * (d % 2) + 1];
-      const float x0 = __uint_as_float(raw[d] << 16), x1 = __uint_as_float(raw[d] & 0xffff0000u);
-      const f32x2 two = {x0 * c - x1 * s, x0 * s + x1 * c};
-      raw[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
-    }
-    f.v[i] = __builtin_bit_cast(bf16x8, raw);
-  }
-}
-__device__ __forceinline__ void turn_frag(Frag<float>& f, const f32x4 (&cs)[4]) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-      const float c = cs[q][e], s = cs[q][e + 1], x0 = f.v[q][e], x1 = f.v[q][e + 1];
-      f.v[q][e] = x0 * c - x1 * s;
-      f.v[q][e + 1] = x0 * s + x1 * c;
-    }
-}
-
-// Values that are not finite, where some rows do not see their key: 0 * Inf would reach those rows.  Such values are taken out of
-// the fragment, and out of 0/1 products over the rows that see the key comes which sums they belong to.
-__device__ __forceinline__ bool frag_finite(const Frag<bf16>& f) {
-  bool ok = true;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
-#pragma unroll
-    for (int d = 0; d < 4; ++d) ok = ok && (w[d] & 0x7f80u) != 0x7f80u && (w[d] & 0x7f800000u) != 0x7f800000u;
-  }
-  return ok;
-}
-__device__ __forceinline__ bool frag_finite(const Frag<float>& f) {
-  bool ok = true;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) ok = ok && (__float_as_uint(f.v[i][j]) & 0x7f800000u) != 0x7f800000u;
-  return ok;
-}
-__device__ __forceinline__ float frag_at(const Frag<bf16>& f, int e) { return (float)f.v[e / 8][e % 8]; }
-__device__ __forceinline__ float frag_at(const Frag<float>& f, int e) { return f.v[e / 4][e % 4]; }
-__device__ __forceinline__ void frag_set(Frag<bf16>& f, int e, float x) { f.v[e / 8][e % 8] = (bf16)x; }
-__device__ __forceinline__ void frag_set(Frag<float>& f, int e, float x) { f.v[e / 4][e % 4] = x; }
-// seen: 1 where the row sees the key; o: the accumulator block of the fragment's 32 channels
-template <typename T> __device__ __forceinline__ void take_nonfinite(Frag<T>& v, const Frag<T>& seen, f32x16& o) {
-  Frag<T> one[3];                                                 // where the value is +Inf, -Inf, NaN
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float x = frag_at(v, e);
-    frag_set(one[0], e, x == INFINITY ? 1.f : 0.f);
-    frag_set(one[1], e, x == -INFINITY ? 1.f : 0.f);
-    frag_set(one[2], e, x != x ? 1.f : 0.f);
-    if (!(x - x == 0.f)) frag_set(v, e, 0.f);
-  }
-  const float what[3] = {INFINITY, -INFINITY, NAN};
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    f32x16 n;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) n[e] = 0.f;
-    mma32(n, one[k], seen);
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (n[e] > 0.f) o[e] += what[k];
-  }
-}
-
-// What the rounding of a probability to bf16 left over, as a second operand: without it that rounding (2^-8 at most) would weigh
-// as much in the result as the result's own
-template <typename T> __device__ __forceinline__ Frag<T> rest_of(const f32x16& pr, const Frag<T>& f) {
-  f32x16 r;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) r[e] = pr[e] - frag_at(f, e);
-  return to_frag<T>(r);
-}
-
-// ---- partial results of the waves of a workgroup, joined through LDS -----------------------------------------------
-template <int D, int W> struct WaveJoin {
-  static constexpr int RE = D + 4;                                // padded row
-  static constexpr size_t bytes(int rows) { return (size_t)W * rows * (RE + 2) * sizeof(float); }
-};
 
 // ------------------------------------------------------------------------------------------------------------------
 // 32 rows a workgroup
@@ -204,10 +105,6 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
     const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = fast_exp2(m_run - m_use);
     m_run = m_new;
-    Frag<T> seen;
-    if (partly)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) frag_set(seen, e, s[e] == -INFINITY ? 0.f : 1.f);
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e] - m_use);
     l_run = block_sum(s, l_run * alpha);
@@ -228,55 +125,23 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
                           : static_cast<const T*>(p.V) + pg * p.v_stride + off * p.rt3;
         frag_set(vf, e, to_f32(src[c]));
       }
-      if (partly && __builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) take_nonfinite<T>(vf, seen, oacc[cb]);
-      mma32(oacc[cb], vf, pf);
-      if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
+      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) {
+        const Frag<T>* v[1] = {&vf};
+        add_by_limit<T, 1>(reinterpret_cast<f32x16(&)[1]>(oacc[cb]), v, pf, &ph, limit, lo, hi, n0, h);
+      } else {
+        mma32(oacc[cb], vf, pf);
+        if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
+      }
     }
   }
 
-  // ---- the waves' sums joined; one row of D channels by D/4 threads ----
-  constexpr int RE = WaveJoin<D, 4>::RE;
-  float* mo = reinterpret_cast<float*>(smem_raw);                 // [4][32][RE], then references and sums [4][32]
-  float* mm = mo + 4 * 32 * RE;
-  float* ml = mm + 4 * 32;
   __syncthreads();                                                // (the plan's words are done with)
-  const float l_tot = halves_sum(l_run);
-  if (h == 0) {
-    mm[wave * 32 + lr] = m_run;
-    ml[wave * 32 + lr] = l_tot;
-  }
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      store4(mo + (wave * 32 + lr) * RE + cb * 32 + 8 * q + 4 * h, oacc[cb][4 * q], oacc[cb][4 * q + 1], oacc[cb][4 * q + 2],
-             oacc[cb][4 * q + 3]);
-  __syncthreads();
   const bool direct = !PREFIX && p.own_parts == 0;
-  for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
-    const int row = i / (D / 4), c = i % (D / 4) * 4;
-    if (rb * 32 + row >= n_rows) break;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, mm[w * 32 + row]);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = mm[w * 32 + row] == -INFINITY ? 0.f : fast_exp2(mm[w * 32 + row] - m);
-      l += f * ml[w * 32 + row];
-      o += f * *reinterpret_cast<const f32x4*>(mo + (w * 32 + row) * RE + c);
-    }
-    const long at = (long)row0 + rb * 32 + row;
-    if (direct) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;                 // no key: the row is zero
-      paged_store4<T>(p, at, c, o * inv);
-      if (c == 0 && p.lse != nullptr) p.lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
-    } else {
-      const long slot = (long)((PREFIX ? 0 : p.prefix_parts) + part) * p.T * p.nH + at;
-      *reinterpret_cast<f32x4*>(p.part_o + slot * D + c) = o;
-      if (c == 0) p.part_ml[slot] = float2{m, l};
-    }
-  }
+  const long row_first = (long)row0 + rb * 32;
+  join_waves<D, 1>(reinterpret_cast<float*>(smem_raw), &oacc, &m_run, &l_run, n_rows - rb * 32, [&](int row, int c, float m, float l, f32x4 o) {
+    if (direct) paged_result<T>(p, row_first + row, c, m, l, o);
+    else paged_partial<D>(p.part_o, p.part_ml, (long)((PREFIX ? 0 : p.prefix_parts) + part) * p.T * p.nH + row_first + row, c, m, l, o);
+  });
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -301,9 +166,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p) {
     l = l * a + ml.y * b;
     o = o * a + v * b;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  paged_store4<T>(p, row, c, o * inv);
-  if (c == 0 && p.lse != nullptr) p.lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+  paged_result<T>(p, row, c, m, l, o);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -313,7 +176,7 @@ int paged_rows_blocks(const PagedArgs& a, int rows) {
 }
 
 template <typename T, int D, bool SH, bool PREFIX> static hipError_t rows_one(const PagedArgs& a, hipStream_t s) {
-  const size_t smem = WaveJoin<D, 4>::bytes(32);
+  const size_t smem = join_bytes<D, 1>();
   auto kern = paged_rows_kernel<T, D, SH, PREFIX>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;

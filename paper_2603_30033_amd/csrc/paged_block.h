@@ -1,0 +1,191 @@
+// Device functions of the attention kernels over pages: operand fragments of cached rows, values that are not finite, partial
+// results of the waves of a workgroup.
+#pragma once
+#include "paged.h"
+
+namespace ta {
+
+// 16 channels c0 .. of a row of r channels (whole 16-byte chunks), zeros behind them
+template <typename T> __device__ __forceinline__ Frag<T> load_frag_upto(const T* row, int c0, int r) {
+  constexpr int CE = 16 / (int)sizeof(T), NC = 16 / CE;
+  Frag<T> f = zero_frag<T>();
+#pragma unroll
+  for (int i = 0; i < NC; ++i)
+    if (c0 + i * CE < r) f.v[i] = *reinterpret_cast<const decltype(f.v[0] + f.v[0])*>(row + c0 + i * CE);
+  return f;
+}
+
+// the fragment's 8 channel pairs turned by the table entries of their 4 quads
+__device__ __forceinline__ void turn_frag(Frag<bf16>& f, const f32x4 (&cs)[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    u32x4 raw = __builtin_bit_cast(u32x4, f.v[i]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const float c = cs[2 * i + d / 2][2 * (d % 2)], s = cs[2 * i + d / 2][2 * (d % 2) + 1];
+      const float x0 = __uint_as_float(raw[d] << 16), x1 = __uint_as_float(raw[d] & 0xffff0000u);
+      const f32x2 two = {x0 * c - x1 * s, x0 * s + x1 * c};
+      raw[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
+    }
+    f.v[i] = __builtin_bit_cast(bf16x8, raw);
+  }
+}
+__device__ __forceinline__ void turn_frag(Frag<float>& f, const f32x4 (&cs)[4]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      const float c = cs[q][e], s = cs[q][e + 1], x0 = f.v[q][e], x1 = f.v[q][e + 1];
+      f.v[q][e] = x0 * c - x1 * s;
+      f.v[q][e + 1] = x0 * s + x1 * c;
+    }
+}
+
+__device__ __forceinline__ float frag_at(const Frag<bf16>& f, int e) { return (float)f.v[e / 8][e % 8]; }
+__device__ __forceinline__ float frag_at(const Frag<float>& f, int e) { return f.v[e / 4][e % 4]; }
+__device__ __forceinline__ void frag_set(Frag<bf16>& f, int e, float x) { f.v[e / 8][e % 8] = (bf16)x; }
+__device__ __forceinline__ void frag_set(Frag<float>& f, int e, float x) { f.v[e / 4][e % 4] = x; }
+
+// Values that are not finite where some rows do not see their key: 0 * Inf in a product would reach those rows.  (Rare; integer
+// arithmetic on the packed words, since as many comparisons as a fragment has elements would each hold a pair of scalar registers.)
+template <typename T> struct Bits;                                // of a 32-bit word that holds one or two elements
+template <> struct Bits<bf16> { static constexpr uint32_t kExp = 0x7f807f80u, kLow = 0x00800080u, kTop = 0x80008000u; };
+template <> struct Bits<float> { static constexpr uint32_t kExp = 0x7f800000u, kLow = 0x00800000u, kTop = 0x80000000u; };
+template <typename T> __device__ __forceinline__ bool frag_finite(const Frag<T>& f) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(Frag<T>) / 16; ++i) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) any |= (w[d] & Bits<T>::kExp) + Bits<T>::kLow;
+  }
+  return (any & Bits<T>::kTop) == 0;
+}
+// f without the elements behind the first `live` of the 32-key block (live as this lane counts: minus 4h)
+__device__ __forceinline__ void frag_upto_key(Frag<bf16>& f, int live) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {                                 // elements 8i + 2d, + 1: keys 8 (e / 4) + e % 4 (+ 4h)
+      const int key = 16 * i + 8 * (d / 2) + 2 * (d % 2);
+      const uint32_t lo = (uint32_t)((key - live) >> 31), hi = (uint32_t)((key + 1 - live) >> 31);
+      w[d] &= (lo & 0xffffu) | (hi & 0xffff0000u);
+    }
+    f.v[i] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+__device__ __forceinline__ void frag_upto_key(Frag<float>& f, int live) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) w[d] &= (uint32_t)((8 * i + d - live) >> 31);
+    f.v[i] = __builtin_bit_cast(f32x4, w);
+  }
+}
+// f without its elements that are not finite
+template <typename T> __device__ __forceinline__ void frag_drop_nonfinite(Frag<T>& f) {
+  constexpr int kShift = sizeof(T) == 2 ? 15 : 31;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(Frag<T>) / 16; ++i) {
+    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      w[d] &= ~(((((w[d] & Bits<T>::kExp) + Bits<T>::kLow) & Bits<T>::kTop) >> kShift) * (sizeof(T) == 2 ? 0xffffu : ~0u));
+    f.v[i] = __builtin_bit_cast(__typeof__(f.v[0] + f.v[0]), w);
+  }
+}
+// O += V P where values are not finite and rows may see different keys of the block that starts at key n0, so that no value reaches
+// a row that does not see it: for the rows of one limit (first .. last) at a time, with the values at and behind the limit taken
+// out; the other rows keep their sums.  bf16: the probabilities' second operand ph, which may be zero or negative, meets the finite
+// values alone (Inf times it would be no Inf).  Rows that see finite values alone get the bits of the plain products.
+template <typename T, int CB>
+__device__ __forceinline__ void add_by_limit(f32x16 (&o)[CB], const Frag<T>* const (&vf)[CB], const Frag<T>& pf, const Frag<T>* ph, int limit,
+                                             int first, int last, int n0, int h) {
+#pragma unroll 1
+  for (int lim = first; lim <= last; ++lim) {
+    const float mine = limit == lim ? 1.f : 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      __builtin_amdgcn_sched_barrier(0);                          // one block at a time: few registers
+      int live = lim - n0 - 4 * h;
+      asm volatile("" : "+v"(live));
+      Frag<T> v = *vf[cb];
+      frag_upto_key(v, live);
+      f32x16 n = o[cb];
+      mma32(n, v, pf);
+      if constexpr (sizeof(T) == 2) {
+        frag_drop_nonfinite(v);
+        mma32(n, v, *ph);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[cb][e] = mine != 0.f ? n[e] : o[cb][e];
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// What the rounding of a probability to bf16 left over, as a second operand: without it that rounding (2^-8 at most) would weigh
+// as much in the result as the result's own
+template <typename T> __device__ __forceinline__ Frag<T> rest_of(const f32x16& pr, const Frag<T>& f) {
+  f32x16 r;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) r[e] = pr[e] - frag_at(f, e);
+  return to_frag<T>(r);
+}
+
+// Join of the partial results of a workgroup's four waves: reference m = max of theirs, sums and outputs scaled by 2^(m_w - m).
+// A wave's lane (row = lane % 32 of block hb, half h) holds channels 32 cb + 8q + 4h + r in o[hb][cb][4q + r]; emit(row, c, m, l,
+// four channels) for every row below `rows`.  The LDS at `lds` must be free and is free again behind the next barrier.
+template <int D, int HB> constexpr size_t join_bytes() { return 4ul * HB * 32 * (D + 4 + 2) * sizeof(float); }
+template <int D, int HB, class Emit>
+__device__ __forceinline__ void join_waves(float* lds, const f32x16 (*o)[D / 32], const float* m_run, const float* l_run, int rows, Emit emit) {
+  constexpr int RE = D + 4, R = HB * 32;                          // padded row; rows
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, h = lane / 32, lr = lane % 32;
+  float* mm = lds + 4 * R * RE;                                   // references and sums [4][R]
+  float* ml = mm + 4 * R;
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) {
+    const float l = halves_sum(l_run[hb]);
+    if (h == 0) {
+      mm[wave * R + hb * 32 + lr] = m_run[hb];
+      ml[wave * R + hb * 32 + lr] = l;
+    }
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store4(lds + (wave * R + hb * 32 + lr) * RE + cb * 32 + 8 * q + 4 * h, o[hb][cb][4 * q], o[hb][cb][4 * q + 1],
+               o[hb][cb][4 * q + 2], o[hb][cb][4 * q + 3]);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * (D / 4); i += 256) {
+    const int row = i / (D / 4), c = i % (D / 4) * 4;
+    if (row >= rows) break;
+    float m = -INFINITY, l = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, mm[w * R + row]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = mm[w * R + row] == -INFINITY ? 0.f : fast_exp2(mm[w * R + row] - m);
+      l += f * ml[w * R + row];
+      v += f * *reinterpret_cast<const f32x4*>(lds + (w * R + row) * RE + c);
+    }
+    emit(row, c, m, l, v);
+  }
+}
+
+// four channels of a finished row (no key: zero, and a log-sum-exp of -infinity) ...
+template <typename T> __device__ __forceinline__ void paged_result(const PagedArgs& p, long row, int c, float m, float l, f32x4 o) {
+  paged_store4<T>(p, row, c, o * (l == 0.f ? 0.f : 1.f / l));
+  if (c == 0 && p.lse != nullptr) p.lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+}
+// ... and of a partial result
+template <int D> __device__ __forceinline__ void paged_partial(float* po, float2* pml, long slot, int c, float m, float l, f32x4 o) {
+  *reinterpret_cast<f32x4*>(po + slot * D + c) = o;
+  if (c == 0) pml[slot] = float2{m, l};
+}
+
+}  // namespace ta

@@ -1,0 +1,421 @@
+// Attention over the paged latent cache for few rows a sequence (bf16, up to 32 (token, head) rows, 64 where the latents are at most 64
+// wide: decode, proposed tokens).
+//
+// The cached rows are read once, in order, and every one serves all heads: 2 nH flops a byte, so HBM bounds it.  What counts is
+// that all compute units stream all the time:
+//   - The key rows of all sequences are cut into units of 128, one behind the other, and every workgroup takes an equal share of
+//     consecutive units, whatever sequences they belong to (it finds its first one by a scan over the lengths).  A share ends
+//     inside a sequence as often as not: such a part leaves (max, sum, output) of its rows, which paged_join adds up.
+//   - Wave w takes keys 32w .. 32w+31 of a unit and does all the work for them (scores of every row, its own running softmax,
+//     product with the values): nothing is shared between the waves while they stream, so there is no barrier in the loop.
+//   - Rows go from the pages straight into the wave's two LDS stages, two units ahead; the page numbers one unit before that.
+#include "paged_block.h"
+
+namespace ta {
+
+constexpr int kUnit = kStreamUnit;      // keys of a unit
+
+// KIND 0: key and value pools; 1: one pool, keys rotated when they are used; 2: one pool, nothing rotated
+template <int D, int KIND> struct StreamLds {
+  static constexpr int kTile = 32 * D;                            // elements of 32 rows
+  static constexpr int kStage = kTile * (KIND == 0 ? 2 : 1) + (KIND == 1 ? 512 : 0);   // KIND 1: 1 KB of rotation entries
+  static constexpr size_t kStages = 4ul * 2 * kStage * sizeof(bf16);
+  static constexpr size_t kRows = KIND == 1 ? (size_t)(D / 4) * 32 * 16 : 0;           // rotation by 0 .. 31, behind the stages
+  template <int HB> static constexpr size_t bytes() {
+    return kStages + kRows > join_bytes<D, HB>() ? kStages + kRows : join_bytes<D, HB>();
+  }
+};
+
+// 16 bytes of zeros, which stand for the channels between a row's end and the tile's width
+__device__ const u32x4 paged_zeros[1] = {{0u, 0u, 0u, 0u}};
+// lane l's 16 bytes at `from` to chunk l of `to` (the same for the whole wave)
+__device__ __forceinline__ void chunk_to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// units of sequence b (no new token: none; no key of its own: one, which leaves its rows' empty result)
+__device__ __forceinline__ int stream_units(const PagedArgs& p, int b) {
+  const PagedSeq s = paged_seq(p, b);
+  return s.nq == 0 ? 0 : max(1, (s.len - p.prefix + kUnit - 1) / kUnit);
+}
+// shares: first unit of workgroup g of G, and the workgroup of unit u; at least kStreamLeast units each
+__device__ __forceinline__ int stream_groups(const PagedArgs& p, int units) {
+  return max(1, min(p.stream_wgs, (units + kStreamLeast - 1) / kStreamLeast));
+}
+__device__ __forceinline__ int stream_first(int g, int units, int G) { return (int)((long)g * units / G); }
+__device__ __forceinline__ int stream_group(int u, int units, int G) { return (int)(((long)(u + 1) * G - 1) / units); }
+
+template <int D, int HB, int KIND>
+// (wide latents: LDS leaves one wave to a SIMD, which may then use all registers)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, HB == 1 && D < 128 ? 2 : 1)))
+void paged_stream_kernel(PagedArgs p) {
+  using T = bf16;
+  using L = StreamLds<D, KIND>;
+  constexpr int CB = D / 32, CPR = D / 8, RPP = 64 / CPR;         // 16-byte chunks of a row, rows of a 1 KB piece
+  constexpr int PIECES = L::kTile / 512;
+  constexpr bool ROT = KIND == 1;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h = lane / 32, lr = lane % 32;
+
+  int b, off, left;                                               // sequence, unit in it, units still to do
+  if (p.stream_wgs == 0) {                                        // a workgroup for every sequence
+    b = blockIdx.x;
+    off = 0;
+    left = stream_units(p, b);
+  } else {
+    int units;
+    b = paged_locate(p.B, 0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
+    if (b < 0) return;
+    const int G = stream_groups(p, units), g = blockIdx.x;
+    if (g >= G) return;
+    const int u0 = stream_first(g, units, G);
+    left = stream_first(g + 1, units, G) - u0;
+    if (u0 > 0) b = paged_locate(p.B, u0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
+  }
+  if (left == 0) return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  off = __builtin_amdgcn_readfirstlane(off);
+
+  T* wbase = reinterpret_cast<T*>(smem_raw) + (long)wave * 2 * L::kStage;
+  f32x4* rowtab = reinterpret_cast<f32x4*>(smem_raw + L::kStages);
+  for (int segment = 0; left > 0; ++segment) {
+    const PagedSeq s = paged_seq(p, b);
+    const int all = stream_units(p, b), cnt = min(left, all - off);
+    const int keys = s.len, n_rows = s.nq * p.nH, row0 = s.q0 * p.nH;
+    const int unit0 = p.prefix + off * kUnit;                     // first key
+    const int* table = p.table + (long)b * p.max_pages;
+    const int lo = p.causal ? keys - s.nq + 1 : keys;             // keys that every row sees
+
+    f32x16 oacc[HB][CB];
+    float m_run[HB], l_run[HB];
+    int limit[HB];                                                // keys that this lane's row sees
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+      m_run[hb] = -INFINITY;
+      l_run[hb] = 0.f;
+      limit[hb] = p.causal ? lo + divide(min(hb * 32 + lr, n_rows - 1), p.heads) : keys;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[hb][cb][e] = 0.f;
+    }
+
+    if (unit0 < keys) {                                           // (the same for the whole workgroup)
+      auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
+      // page number of this lane's row of block j; rows behind the last repeat it and are masked
+      auto page_at = [&](int j) {
+        const int n = min(block_at(j) + lr, keys - 1);
+        return paged_page(table, min(divide(n, p.ps), p.max_pages - 1), p.n_pages);
+      };
+      auto issue = [&](int j, int st, int page) {
+        const int n0 = block_at(j);
+        const int n = min(n0 + lr, keys - 1), at = n - divide(n, p.ps) * p.page_size;
+        T* kt = wbase + (long)st * L::kStage;
+        int l = lane;
+        asm volatile("" : "+v"(l));                               // (rows and chunks of the pieces are formed afresh, not kept across the loop)
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+          const int row = q * RPP + l / CPR, c = ((l % CPR) ^ swz_x<CPR>(row)) * 8;
+          const long pg = __shfl(page, row), a = __shfl(at, row);
+          const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3 + c;
+          chunk_to_lds(c < p.r3 ? kp : reinterpret_cast<const T*>(paged_zeros), kt + q * 512);
+          if constexpr (KIND == 0) {
+            const T* vp = static_cast<const T*>(p.V) + pg * p.v_stride + a * p.rt3 + c;
+            chunk_to_lds(c < p.rt3 ? vp : reinterpret_cast<const T*>(paged_zeros), kt + L::kTile + q * 512);
+          }
+        }
+        if constexpr (ROT) {
+          const f32x4* tab = reinterpret_cast<const f32x4*>(p.rope) + (long)min(lr, D / 4 - 1) * p.rope_ld + min(n0, p.rope_ld - 1);
+          chunk_to_lds(tab, kt + L::kTile);
+        }
+      };
+      // vector-memory operations of one stage and the page numbers fetched with it
+      constexpr int OPS = PIECES * (KIND == 0 ? 2 : 1) + (ROT ? 1 : 0) + 1;
+
+      int page = page_at(0);
+      Frag<T> qf[HB][CB];
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb) {
+        const T* q = static_cast<const T*>(p.Q) + (long)(row0 + min(hb * 32 + lr, n_rows - 1)) * p.q_row;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) qf[hb][cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
+      }
+      if constexpr (ROT) {
+        for (int i = threadIdx.x; i < (D / 4) * 32; i += 256)
+          rowtab[i] = reinterpret_cast<const f32x4*>(p.rope)[(long)(i / 32) * p.rope_ld + min(i % 32, p.rope_ld - 1)];
+      }
+      int next = page_at(1);
+      wait_vm<0>();                                               // plain loads out of the way of the counted ones
+      wait_lds();
+      if constexpr (ROT) __syncthreads();
+      issue(0, 0, page);
+      page = page_at(2);
+      issue(1, 1, next);
+      next = page_at(3);
+
+      constexpr float kLazy = 8.f;
+      const int xs = swz_x<CPR>(lr);
+      auto round = [&](int j, int st, int ids) {
+        const int n0 = block_at(j);
+        const T* kt = wbase + (long)st * L::kStage;
+        wait_vm<OPS>();
+        f32x16 sc[HB];
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[hb][e] = 0.f;
+        if constexpr (ROT) {
+          const f32x4* rl = reinterpret_cast<const f32x4*>(kt + L::kTile);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            const Frag<T> raw = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
+            f32x16 x;                                             // the row's 16 channels, turned by (first key of the block) + (row)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 t = rl[8 * cb + 4 * h + q], a = rowtab[(8 * cb + 4 * h + q) * 32 + lr];
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const float c = a[e] * t[e] - a[e + 1] * t[e + 1], sn = a[e + 1] * t[e] + a[e] * t[e + 1];
+                const float x0 = frag_at(raw, 4 * q + e), x1 = frag_at(raw, 4 * q + e + 1);
+                x[4 * q + e] = x0 * c - x1 * sn;
+                x[4 * q + e + 1] = x0 * sn + x1 * c;
+              }
+            }
+            const Frag<T> kf = to_frag<T>(x), rest = rest_of<T>(x, kf);
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) {
+              mma32(sc[hb], kf, qf[hb][cb]);
+              mma32(sc[hb], rest, qf[hb][cb]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            const Frag<T> kf = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) mma32(sc[hb], kf, qf[hb][cb]);
+          }
+        }
+        // the value fragments (transposing reads) are taken before the stage is filled again
+        constexpr int TF = CB < 2 ? 1 : 2;
+        Frag<T> vf[CB / TF][TF];
+#pragma unroll
+        for (int k = 0; k < CB / TF; ++k) load_frags_tr_swz<CPR, false>(vf[k], kt + (KIND == 0 ? L::kTile : 0), 0, k * TF * 32, lane);
+        wait_lds();
+        issue(j + 2, st, ids);
+
+        const bool partly = n0 + 32 > lo;
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[hb][e] *= p.scale;
+          if (partly)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[hb][e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit[hb] ? sc[hb][e] : -INFINITY;
+        }
+        // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the
+        // reference by more than kLazy (probabilities stay below 2^kLazy)
+        Frag<T> pf[HB], ph[HB];
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[hb][e]);
+          mx = halves_max(mx);
+          const bool raise = mx > m_run[hb] + kLazy;              // -inf + kLazy = -inf: the first block with a key raises
+          if (__builtin_amdgcn_ballot_w64(raise) != 0ull) {
+            const float alpha = raise ? fast_exp2(m_run[hb] - mx) : 1.f;
+            if (raise) m_run[hb] = mx;
+            l_run[hb] *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) oacc[hb][cb][e] *= alpha;
+          }
+          const float m_use = m_run[hb] == -INFINITY ? 0.f : m_run[hb];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[hb][e] = fast_exp2(sc[hb][e] - m_use);
+          l_run[hb] = block_sum(sc[hb], l_run[hb]);
+          pf[hb] = to_frag<T>(sc[hb]);
+          ph[hb] = rest_of<T>(sc[hb], pf[hb]);
+        }
+        bool fine = true;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) fine = fine && frag_finite(vf[cb / TF][cb % TF]);
+        if (__builtin_amdgcn_ballot_w64(!fine) == 0ull) {
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb) {
+              mma32(oacc[hb][cb], vf[cb / TF][cb % TF], pf[hb]);
+              mma32(oacc[hb][cb], vf[cb / TF][cb % TF], ph[hb]);
+            }
+        } else {
+          const Frag<T>* v[CB];
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) v[cb] = &vf[cb / TF][cb % TF];
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) add_by_limit<T, CB>(oacc[hb], v, pf[hb], &ph[hb], limit[hb], lo, keys, n0, h);
+        }
+      };
+      for (int j = 0; j < cnt; ++j) {
+        const int after = page_at(j + 4);
+        round(j, j & 1, page);
+        page = next;
+        next = after;
+      }
+      wait_vm<0>();                                               // tiles requested past the end still land in LDS
+    }
+    __syncthreads();
+
+    const bool complete = off == 0 && cnt == all, direct = complete && p.prefix_parts == 0;
+    const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (2l * blockIdx.x + (segment > 0)) * (HB * 32);
+    float* po = complete ? p.part_o : p.stream_o;
+    float2* pml = complete ? p.part_ml : p.stream_ml;
+    join_waves<D, HB>(reinterpret_cast<float*>(smem_raw), oacc, m_run, l_run, n_rows, [&](int row, int c, float m, float l, f32x4 o) {
+      if (direct) paged_result<T>(p, (long)row0 + row, c, m, l, o);
+      else paged_partial<D>(po, pml, slot0 + row, c, m, l, o);
+    });
+    left -= cnt;
+    if (left > 0) {
+      off = 0;
+      do ++b;
+      while (stream_units(p, b) == 0);                            // (units are left, so a sequence with some follows)
+      __syncthreads();
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// The partial results of a sequence's rows: those of the prefix, and its own.  Grid: sequences x groups of rows; a row by D/4
+// threads, as many rows a workgroup as leave every part of a row a group of threads of its own (up to 8 groups).
+// ------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups) {
+  using T = bf16;
+  constexpr int L = D / 4, SLOTS = 256 / L;                       // threads of a row, rows or groups of a workgroup
+  __shared__ int sums[8];
+  __shared__ float4 po[256];
+  __shared__ float2 pml[SLOTS];
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const PagedSeq s = paged_seq(p, b);
+  const int n_rows = s.nq * p.nH, per = SLOTS / groups;
+  if ((int)blockIdx.y * per >= n_rows) return;
+
+  int g0 = 0, g1 = 0, u0 = 0, units = 0, G = 1;                   // workgroups that share the sequence
+  if (p.stream_wgs > 0) {
+    int before = 0, all = 0;
+    for (int i = tid; i < p.B; i += 256) {
+      const int n = stream_units(p, i);
+      all += n;
+      if (i < b) before += n;
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      all += __shfl_xor(all, d);
+      before += __shfl_xor(before, d);
+    }
+    if (tid % kWave == 0) {
+      sums[tid / kWave] = all;
+      sums[4 + tid / kWave] = before;
+    }
+    __syncthreads();
+    units = sums[0] + sums[1] + sums[2] + sums[3];
+    u0 = sums[4] + sums[5] + sums[6] + sums[7];
+    G = stream_groups(p, units);
+    g0 = stream_group(u0, units, G);
+    g1 = stream_group(u0 + stream_units(p, b) - 1, units, G);
+  }
+  const bool complete = g0 == g1;                                 // one workgroup did it all
+  if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
+  const int parts = p.prefix_parts + (g1 - g0 + 1);
+  const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
+  const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + r;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (r < n_rows) {
+    constexpr int U = 8;                                          // parts whose loads are in flight together
+    for (int i0 = group; i0 < parts; i0 += U * groups) {
+      float2 ml[U];
+      f32x4 v[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int i = min(i0 + k * groups, parts - 1), g = g0 + i - p.prefix_parts;
+        const bool by_row = i < p.prefix_parts || complete;
+        const long at = by_row ? i * rows + row : (2l * g + (stream_first(g, units, G) < u0)) * (p.hb * 32) + r;
+        ml[k] = (by_row ? p.part_ml : p.stream_ml)[at];
+        v[k] = *reinterpret_cast<const f32x4*>((by_row ? p.part_o : p.stream_o) + at * D + c);
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (i0 + k * groups >= parts || ml[k].x == -INFINITY) continue;
+        const float top = fmaxf(m, ml[k].x), a = fast_exp2(m - top), f = fast_exp2(ml[k].x - top);
+        m = top;
+        l = l * a + ml[k].y * f;
+        o = o * a + v[k] * f;
+      }
+    }
+  }
+  if (groups > 1) {                                               // the groups' sums, in their order
+    po[tid] = float4{o[0], o[1], o[2], o[3]};
+    if (c == 0) pml[slot] = float2{m, l};
+    __syncthreads();
+    if (group > 0) return;
+    for (int k = 1; k < groups; ++k) {
+      const float2 ml = pml[slot + k * per];
+      if (ml.x == -INFINITY) continue;
+      const float4 v = po[tid + k * per * L];
+      const float top = fmaxf(m, ml.x), a = fast_exp2(m - top), f = fast_exp2(ml.x - top);
+      m = top;
+      l = l * a + ml.y * f;
+      o = o * a + f32x4{v.x, v.y, v.z, v.w} * f;
+    }
+  }
+  if (r < n_rows) paged_result<T>(p, row, c, m, l, o);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+template <int D, int HB, int KIND> static hipError_t stream_one(const PagedArgs& a, hipStream_t s) {
+  const size_t smem = StreamLds<D, KIND>::template bytes<HB>();
+  auto kern = paged_stream_kernel<D, HB, KIND>;
+  static LdsOnce lds_once;                                       // one per kernel instantiation
+  if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3(a.stream_wgs > 0 ? a.stream_wgs : a.B), dim3(256), smem, s, a);
+  return hipGetLastError();
+}
+template <int D> static hipError_t stream_variant(const PagedArgs& a, hipStream_t s) {
+  const int kind = !a.shared_kv ? 0 : a.rope != nullptr ? 1 : 2;
+  if (a.hb == 1) return kind == 0 ? stream_one<D, 1, 0>(a, s) : kind == 1 ? stream_one<D, 1, 1>(a, s) : stream_one<D, 1, 2>(a, s);
+  if constexpr (D < 128) return kind == 0 ? stream_one<D, 2, 0>(a, s) : kind == 1 ? stream_one<D, 2, 1>(a, s) : stream_one<D, 2, 2>(a, s);
+  return hipErrorInvalidValue;                                    // (two blocks of 128 channels do not fit the registers)
+}
+hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s) {
+  switch (a.D) {
+    case 32: return stream_variant<32>(a, s);
+    case 64: return stream_variant<64>(a, s);
+    case 128: return stream_variant<128>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int D> static hipError_t join_one(const PagedArgs& a, hipStream_t s) {
+  constexpr int SLOTS = 256 / (D / 4);
+  // parts that a sequence has on average: that many groups of threads share a row's
+  const int parts = a.prefix_parts + (a.stream_wgs > 0 ? a.stream_wgs / a.B : 0) + 1;
+  int groups = 1;
+  while (groups < 8 && 4 * groups < parts) groups *= 2;
+  const int per = SLOTS / groups, most = a.max_new * a.nH;
+  hipLaunchKernelGGL(paged_join_kernel<D>, dim3(a.B, (most + per - 1) / per), dim3(256), 0, s, a, groups);
+  return hipGetLastError();
+}
+hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s) {
+  switch (a.D) {
+    case 32: return join_one<32>(a, s);
+    case 64: return join_one<64>(a, s);
+    case 128: return join_one<128>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace ta
