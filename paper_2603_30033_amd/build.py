@@ -12,7 +12,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtucker_attn.so")
 SOURCES = ["api.hip", "prep.hip", "gemm.hip", "out_proj.hip", "attn_prefill.hip", "attn_merge.hip", "attn_decode.hip",
            "attn_bwd.hip", "gemm_tn.hip", "bwd_misc.hip", "convert.hip", "eigen.hip", "ceiling.hip", "decode_proj.hip",
-           "paged_append.hip", "paged_attn.hip", "paged_stream.hip", "paged_api.hip"]
+           "paged_append.hip", "paged_attn.hip", "paged_stream.hip", "paged_tile.hip",
+           "paged_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed fp32 instructions are kept off: scalar fp32 code must not be fused into them
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

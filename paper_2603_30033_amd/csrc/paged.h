@@ -71,9 +71,11 @@ struct PagedAppendArgs {
 
 int paged_rows_blocks(const PagedArgs& a, int rows);   // row blocks of `rows` rows that a batch can have
 hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s);
-hipError_t launch_paged_rows(int dtype, const PagedArgs& a, bool prefix_pass, hipStream_t s);
+hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // fp32
 hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16
 hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s);     // of its partial results, and the prefix's
+hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // bf16
+constexpr int kTileWaves = 4;          // waves of paged_tile with rows of their own
 hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s);
 
 // ---- device -----------------------------------------------------------------------------------------------------
@@ -93,18 +95,15 @@ template <typename A> __device__ __forceinline__ PagedSeq paged_seq(const A& p, 
   return s;
 }
 
-// Page of row n (n / page size = i) by a table of `entries` entries; a number that is no page of the pool reads page 0
-__device__ __forceinline__ int paged_page(const int* table, int i, int n_pages) {
-  const int page = table[i];
-  return (uint32_t)page < (uint32_t)n_pages ? page : 0;
-}
+// Page of a table entry; a number that is no page of the pool reads page 0
+__device__ __forceinline__ int paged_page(int entry, int n_pages) { return (uint32_t)entry < (uint32_t)n_pages ? entry : 0; }
 
 // Which sequence item `target` belongs to when every sequence has items(b) of them, one behind the other: its number (-1: behind
-// the last), the item's index in it, and the number of all items.  All 256 threads call; `sh` holds 8 words.
-template <class F>
+// the last), the item's index in it, and the number of all items.  All NT threads call; `sh` holds NT / 64 + 2 words.
+template <int NT = 256, class F>
 __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh, int& index, int& total) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int per = (B + 255) / 256, first = tid * per, last = min(B, first + per);
+  const int per = (B + NT - 1) / NT, first = tid * per, last = min(B, first + per);
   int mine = 0;
   for (int b = first; b < last; ++b) mine += items(b);
   int x = mine;
@@ -113,21 +112,26 @@ __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh,
     const int y = __shfl_up(x, d);
     if (lane >= d) x += y;
   }
+  constexpr int W = NT / kWave;
   if (lane == kWave - 1) sh[wave] = x;
-  if (tid == 0) sh[4] = -1;
+  if (tid == 0) sh[W] = -1;
   __syncthreads();
-  total = sh[0] + sh[1] + sh[2] + sh[3];
   int before = x - mine;
-  for (int w = 0; w < wave; ++w) before += sh[w];
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    total += sh[w];
+    before += w < wave ? sh[w] : 0;
+  }
   if (target >= before && target < before + mine) {
     int b = first;
     for (int n; target >= before + (n = items(b)); ++b) before += n;
-    sh[4] = b;
-    sh[5] = target - before;
+    sh[W] = b;
+    sh[W + 1] = target - before;
   }
   __syncthreads();
-  index = sh[5];
-  const int found = sh[4];
+  index = sh[W + 1];
+  const int found = sh[W];
   __syncthreads();
   return found;
 }

@@ -43,10 +43,10 @@ template <typename A> void fill(A& a, const tucker_attn_ctx* c, const tucker_att
   a.rope = c->rope; a.rope_ld = f.max_positions;
 }
 
-// Parts that the keys of a product of `blocks` row blocks are dealt to: two workgroups for every compute unit, and no part of
-// fewer than 128 keys
-int key_parts(const tucker_attn_ctx* c, long blocks, int keys) {
-  const long most = (keys + 127) / 128, want = 2l * c->n_cus / (blocks < 1 ? 1 : blocks);
+// Parts that the keys of a product of `blocks` row blocks are dealt to: `wgs` workgroups for every compute unit, and no part of
+// fewer than `least` keys
+int key_parts(const tucker_attn_ctx* c, long blocks, int keys, int wgs, int least) {
+  const long most = (keys + least - 1) / least, want = (long)wgs * c->n_cus / (blocks < 1 ? 1 : blocks);
   return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
@@ -60,13 +60,15 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const long rows = (long)b->T * f.n_heads, most = (long)b->max_new * f.n_heads;
   const int keys = b->max_len - prefix;
   a.hb = f.dtype != TUCKER_ATTN_BF16 ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
-  a.prefix_parts = prefix > 0 ? key_parts(c, (rows + 31) / 32, prefix) : 0;
+  const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // paged_tile: fp32 rows go through paged_rows
+  const int block = tile ? 32 * kTileWaves : 32, wgs = tile ? 1 : 2, least = tile ? 256 : 128;
+  a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, wgs, least) : 0;
   a.stream_wgs = 0;
   if (a.hb > 0) {
     a.own_parts = prefix > 0 ? 1 : 0;                             // sequences that one workgroup does alone
     if (keys > kStreamWhole) a.stream_wgs = c->n_cus;
   } else {
-    a.own_parts = key_parts(c, paged_rows_blocks(a, 32), keys);
+    a.own_parts = key_parts(c, paged_rows_blocks(a, block), keys, wgs, least);
     if (a.own_parts == 1 && prefix == 0) a.own_parts = 0;
   }
   const size_t parts = a.prefix_parts + a.own_parts, shared = 2ul * a.stream_wgs * a.hb * 32;
@@ -99,11 +101,13 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
   if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  const bool tile = f.dtype == TUCKER_ATTN_BF16;
   if (prefix > 0) {
-    if (launch_paged_rows(f.dtype, a, true, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+    if ((tile ? launch_paged_tile(a, true, s) : launch_paged_rows(a, true, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("prefix_attention");
   }
-  if ((a.hb > 0 ? launch_paged_stream(a, s) : launch_paged_rows(f.dtype, a, false, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if ((a.hb > 0 ? launch_paged_stream(a, s) : tile ? launch_paged_tile(a, false, s) : launch_paged_rows(a, false, s)) != hipSuccess)
+    return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("paged_attention");
   if (a.prefix_parts + a.own_parts + a.stream_wgs > 0) {
     if ((a.hb > 0 ? launch_paged_join(a, s) : launch_paged_merge(f.dtype, a, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
     const int n0 = first + k * 32;
     const int n = min(n0 + lr, hi - 1);                           // keys behind the last repeat it and are masked
     const int pi = divide(n, p.ps);
-    const int page = paged_page(table, min(pi, pages - 1), p.n_pages), at = n - pi * p.page_size;
+    const int page = paged_page(table[min(pi, pages - 1)], p.n_pages), at = n - pi * p.page_size;
     const T* krow = static_cast<const T*>(p.K) + page * p.k_stride + (long)at * p.r3;
     f32x16 s;
 #pragma unroll
@@ -125,13 +125,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
                           : static_cast<const T*>(p.V) + pg * p.v_stride + off * p.rt3;
         frag_set(vf, e, to_f32(src[c]));
       }
-      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) {
-        const Frag<T>* v[1] = {&vf};
-        add_by_limit<T, 1>(reinterpret_cast<f32x16(&)[1]>(oacc[cb]), v, pf, &ph, limit, lo, hi, n0, h);
-      } else {
-        mma32(oacc[cb], vf, pf);
-        if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
-      }
+      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) take_nonfinite<T>(vf, frag_seen(limit - n0 - 4 * h, T()), oacc[cb]);
+      mma32(oacc[cb], vf, pf);
+      if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
     }
   }
 
@@ -196,9 +192,7 @@ template <typename T> static hipError_t rows_dispatch(const PagedArgs& a, bool p
   }
   return hipErrorInvalidValue;
 }
-hipError_t launch_paged_rows(int dtype, const PagedArgs& a, bool prefix_pass, hipStream_t s) {
-  return dtype == 0 ? rows_dispatch<float>(a, prefix_pass, s) : rows_dispatch<bf16>(a, prefix_pass, s);
-}
+hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s) { return rows_dispatch<float>(a, prefix_pass, s); }
 
 template <typename T> static hipError_t merge_dispatch(const PagedArgs& a, hipStream_t s) {
   const long rows = (long)a.T * a.nH;

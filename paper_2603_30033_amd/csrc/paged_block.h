@@ -46,11 +46,21 @@ __device__ __forceinline__ float frag_at(const Frag<float>& f, int e) { return f
 __device__ __forceinline__ void frag_set(Frag<bf16>& f, int e, float x) { f.v[e / 8][e % 8] = (bf16)x; }
 __device__ __forceinline__ void frag_set(Frag<float>& f, int e, float x) { f.v[e / 4][e % 4] = x; }
 
-// Values that are not finite where some rows do not see their key: 0 * Inf in a product would reach those rows.  (Rare; integer
-// arithmetic on the packed words, since as many comparisons as a fragment has elements would each hold a pair of scalar registers.)
+// Values that are not finite where some rows do not see their key: 0 * Inf in a product would reach those rows.  Such values are taken
+// out of the operand, and one product of small numbers that stand for them with 0/1 (the row sees the key) says which sums they
+// belong to.  The other sums get the bits of the plain product.  (Rare; integer arithmetic on the packed words, since as many
+// comparisons as a fragment has elements would each hold a pair of scalar registers.)
 template <typename T> struct Bits;                                // of a 32-bit word that holds one or two elements
-template <> struct Bits<bf16> { static constexpr uint32_t kExp = 0x7f807f80u, kLow = 0x00800080u, kTop = 0x80008000u; };
-template <> struct Bits<float> { static constexpr uint32_t kExp = 0x7f800000u, kLow = 0x00800000u, kTop = 0x80000000u; };
+template <> struct Bits<bf16> {
+  static constexpr uint32_t kExp = 0x7f807f80u, kLow = 0x00800080u, kTop = 0x80008000u, kMant = 0x007f007fu, kUnit = 0x00010001u, kAll = 0xffffu;
+  static constexpr int kSign = 15, kMantBits = 7;
+  static constexpr uint32_t kPlus = 0x3f80u, kMinus = 0x3a80u, kNan = 0x4480u;        // 1, 2^-10, 2^10
+};
+template <> struct Bits<float> {
+  static constexpr uint32_t kExp = 0x7f800000u, kLow = 0x00800000u, kTop = 0x80000000u, kMant = 0x007fffffu, kUnit = 1u, kAll = ~0u;
+  static constexpr int kSign = 31, kMantBits = 23;
+  static constexpr uint32_t kPlus = 0x3f800000u, kMinus = 0x3a800000u, kNan = 0x44800000u;
+};
 template <typename T> __device__ __forceinline__ bool frag_finite(const Frag<T>& f) {
   uint32_t any = 0;
 #pragma unroll
@@ -61,67 +71,59 @@ template <typename T> __device__ __forceinline__ bool frag_finite(const Frag<T>&
   }
   return (any & Bits<T>::kTop) == 0;
 }
-// f without the elements behind the first `live` of the 32-key block (live as this lane counts: minus 4h)
-__device__ __forceinline__ void frag_upto_key(Frag<bf16>& f, int live) {
+// 1 for the keys of a block that the row sees: `live` of them, as this lane counts (minus 4h)
+__device__ __forceinline__ Frag<bf16> frag_seen(int live, bf16) {
+  Frag<bf16> f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+    u32x4 w;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {                                 // elements 8i + 2d, + 1: keys 8 (e / 4) + e % 4 (+ 4h)
       const int key = 16 * i + 8 * (d / 2) + 2 * (d % 2);
-      const uint32_t lo = (uint32_t)((key - live) >> 31), hi = (uint32_t)((key + 1 - live) >> 31);
-      w[d] &= (lo & 0xffffu) | (hi & 0xffff0000u);
+      w[d] = ((uint32_t)((key - live) >> 31) & 0x3f80u) | ((uint32_t)((key + 1 - live) >> 31) & 0x3f800000u);
     }
     f.v[i] = __builtin_bit_cast(bf16x8, w);
   }
+  return f;
 }
-__device__ __forceinline__ void frag_upto_key(Frag<float>& f, int live) {
+__device__ __forceinline__ Frag<float> frag_seen(int live, float) {
+  Frag<float> f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+    u32x4 w;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) w[d] &= (uint32_t)((8 * i + d - live) >> 31);
+    for (int d = 0; d < 4; ++d) w[d] = (uint32_t)((8 * i + d - live) >> 31) & 0x3f800000u;
     f.v[i] = __builtin_bit_cast(f32x4, w);
   }
+  return f;
 }
-// f without its elements that are not finite
-template <typename T> __device__ __forceinline__ void frag_drop_nonfinite(Frag<T>& f) {
-  constexpr int kShift = sizeof(T) == 2 ? 15 : 31;
+// v without its elements that are not finite, which go to the sums o of its 32 channels and of the rows that see their key
+template <typename T> __device__ __forceinline__ void take_nonfinite(Frag<T>& v, const Frag<T>& seen, f32x16& o) {
+  using B = Bits<T>;
+  __builtin_amdgcn_sched_barrier(0);                              // (one fragment at a time: few registers)
+  Frag<T> stand;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(Frag<T>) / 16; ++i) {
-    u32x4 w = __builtin_bit_cast(u32x4, f.v[i]);
+    u32x4 w = __builtin_bit_cast(u32x4, v.v[i]), x;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-      w[d] &= ~(((((w[d] & Bits<T>::kExp) + Bits<T>::kLow) & Bits<T>::kTop) >> kShift) * (sizeof(T) == 2 ? 0xffffu : ~0u));
-    f.v[i] = __builtin_bit_cast(__typeof__(f.v[0] + f.v[0]), w);
-  }
-}
-// O += V P where values are not finite and rows may see different keys of the block that starts at key n0, so that no value reaches
-// a row that does not see it: for the rows of one limit (first .. last) at a time, with the values at and behind the limit taken
-// out; the other rows keep their sums.  bf16: the probabilities' second operand ph, which may be zero or negative, meets the finite
-// values alone (Inf times it would be no Inf).  Rows that see finite values alone get the bits of the plain products.
-template <typename T, int CB>
-__device__ __forceinline__ void add_by_limit(f32x16 (&o)[CB], const Frag<T>* const (&vf)[CB], const Frag<T>& pf, const Frag<T>* ph, int limit,
-                                             int first, int last, int n0, int h) {
-#pragma unroll 1
-  for (int lim = first; lim <= last; ++lim) {
-    const float mine = limit == lim ? 1.f : 0.f;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      __builtin_amdgcn_sched_barrier(0);                          // one block at a time: few registers
-      int live = lim - n0 - 4 * h;
-      asm volatile("" : "+v"(live));
-      Frag<T> v = *vf[cb];
-      frag_upto_key(v, live);
-      f32x16 n = o[cb];
-      mma32(n, v, pf);
-      if constexpr (sizeof(T) == 2) {
-        frag_drop_nonfinite(v);
-        mma32(n, v, *ph);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) o[cb][e] = mine != 0.f ? n[e] : o[cb][e];
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t bad = (((w[d] & B::kExp) + B::kLow) >> B::kSign) & B::kUnit;
+      const uint32_t nan = (((w[d] & B::kMant) + B::kMant) >> B::kMantBits) & bad, minus = (w[d] >> B::kSign) & bad & ~nan;
+      x[d] = nan * B::kNan + minus * B::kMinus + (bad & ~nan & ~minus) * B::kPlus;
+      w[d] &= ~(bad * B::kAll);
     }
+    v.v[i] = __builtin_bit_cast(__typeof__(v.v[0] + v.v[0]), w);
+    stand.v[i] = __builtin_bit_cast(__typeof__(v.v[0] + v.v[0]), x);
+  }
+  f32x16 n;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) n[e] = 0.f;
+  mma32(n, stand, seen);                                          // up to 32 of each kind: exact
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    o[e] += n[e] >= 1.f ? INFINITY : 0.f;
+    o[e] += __builtin_amdgcn_fractf(n[e]) > 0.f ? -INFINITY : 0.f;
+    o[e] += n[e] >= 1024.f ? NAN : 0.f;
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -133,6 +135,16 @@ template <typename T> __device__ __forceinline__ Frag<T> rest_of(const f32x16& p
 #pragma unroll
   for (int e = 0; e < 16; ++e) r[e] = pr[e] - frag_at(f, e);
   return to_frag<T>(r);
+}
+
+// 16 bytes of zeros, which stand for the channels between a row's end and the tile's width
+static __device__ const u32x4 paged_zeros[1] = {{0u, 0u, 0u, 0u}};
+// lane l's 16 bytes (4 bytes) at `from` to chunk (word) l of `to` (the same for the whole wave)
+__device__ __forceinline__ void word_to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+__device__ __forceinline__ void chunk_to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
 // Join of the partial results of a workgroup's four waves: reference m = max of theirs, sums and outputs scaled by 2^(m_w - m).

@@ -21,17 +21,10 @@ template <int D, int KIND> struct StreamLds {
   static constexpr int kStage = kTile * (KIND == 0 ? 2 : 1) + (KIND == 1 ? 512 : 0);   // KIND 1: 1 KB of rotation entries
   static constexpr size_t kStages = 4ul * 2 * kStage * sizeof(bf16);
   static constexpr size_t kRows = KIND == 1 ? (size_t)(D / 4) * 32 * 16 : 0;           // rotation by 0 .. 31, behind the stages
-  template <int HB> static constexpr size_t bytes() {
-    return kStages + kRows > join_bytes<D, HB>() ? kStages + kRows : join_bytes<D, HB>();
-  }
+  static constexpr size_t kEntries = 4ul * 4 * 64 * sizeof(int);  // table entries of four blocks a wave, behind those
+  static constexpr size_t kAll = kStages + kRows + kEntries;
+  template <int HB> static constexpr size_t bytes() { return kAll > join_bytes<D, HB>() ? kAll : join_bytes<D, HB>(); }
 };
-
-// 16 bytes of zeros, which stand for the channels between a row's end and the tile's width
-__device__ const u32x4 paged_zeros[1] = {{0u, 0u, 0u, 0u}};
-// lane l's 16 bytes at `from` to chunk l of `to` (the same for the whole wave)
-__device__ __forceinline__ void chunk_to_lds(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
 
 // units of sequence b (no new token: none; no key of its own: one, which leaves its rows' empty result)
 __device__ __forceinline__ int stream_units(const PagedArgs& p, int b) {
@@ -79,6 +72,7 @@ void paged_stream_kernel(PagedArgs p) {
 
   T* wbase = reinterpret_cast<T*>(smem_raw) + (long)wave * 2 * L::kStage;
   f32x4* rowtab = reinterpret_cast<f32x4*>(smem_raw + L::kStages);
+  int* entries = reinterpret_cast<int*>(smem_raw + L::kStages + L::kRows) + wave * 4 * 64;
   for (int segment = 0; left > 0; ++segment) {
     const PagedSeq s = paged_seq(p, b);
     const int all = stream_units(p, b), cnt = min(left, all - off);
@@ -103,21 +97,23 @@ void paged_stream_kernel(PagedArgs p) {
 
     if (unit0 < keys) {                                           // (the same for the whole workgroup)
       auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
-      // page number of this lane's row of block j; rows behind the last repeat it and are masked
-      auto page_at = [&](int j) {
+      // The table entries of block j's rows come by way of LDS too: an entry in a register would be waited for with every tile
+      // behind it.  Rows behind the last repeat it and are masked.
+      auto fetch_entries = [&](int j) {
         const int n = min(block_at(j) + lr, keys - 1);
-        return paged_page(table, min(divide(n, p.ps), p.max_pages - 1), p.n_pages);
+        word_to_lds(table + min(divide(n, p.ps), p.max_pages - 1), entries + (j & 3) * 64);
       };
-      auto issue = [&](int j, int st, int page) {
+      auto issue = [&](int j, int st) {
         const int n0 = block_at(j);
-        const int n = min(n0 + lr, keys - 1), at = n - divide(n, p.ps) * p.page_size;
+        const int* ids = entries + (j & 3) * 64;
         T* kt = wbase + (long)st * L::kStage;
         int l = lane;
         asm volatile("" : "+v"(l));                               // (rows and chunks of the pieces are formed afresh, not kept across the loop)
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) {
           const int row = q * RPP + l / CPR, c = ((l % CPR) ^ swz_x<CPR>(row)) * 8;
-          const long pg = __shfl(page, row), a = __shfl(at, row);
+          const int n = min(n0 + row, keys - 1);
+          const long pg = paged_page(ids[row], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
           const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3 + c;
           chunk_to_lds(c < p.r3 ? kp : reinterpret_cast<const T*>(paged_zeros), kt + q * 512);
           if constexpr (KIND == 0) {
@@ -130,10 +126,12 @@ void paged_stream_kernel(PagedArgs p) {
           chunk_to_lds(tab, kt + L::kTile);
         }
       };
-      // vector-memory operations of one stage and the page numbers fetched with it
-      constexpr int OPS = PIECES * (KIND == 0 ? 2 : 1) + (ROT ? 1 : 0) + 1;
+      // vector-memory operations behind those of block j when round j begins: entries, a stage, entries
+      constexpr int OPS = PIECES * (KIND == 0 ? 2 : 1) + (ROT ? 1 : 0) + 2;
 
-      int page = page_at(0);
+      fetch_entries(0);
+      fetch_entries(1);
+      fetch_entries(2);
       Frag<T> qf[HB][CB];
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb) {
@@ -145,18 +143,16 @@ void paged_stream_kernel(PagedArgs p) {
         for (int i = threadIdx.x; i < (D / 4) * 32; i += 256)
           rowtab[i] = reinterpret_cast<const f32x4*>(p.rope)[(long)(i / 32) * p.rope_ld + min(i % 32, p.rope_ld - 1)];
       }
-      int next = page_at(1);
-      wait_vm<0>();                                               // plain loads out of the way of the counted ones
+      wait_vm<0>();                                               // entries, and plain loads out of the way of the counted ones
       wait_lds();
       if constexpr (ROT) __syncthreads();
-      issue(0, 0, page);
-      page = page_at(2);
-      issue(1, 1, next);
-      next = page_at(3);
+      issue(0, 0);
+      fetch_entries(3);
+      issue(1, 1);
 
       constexpr float kLazy = 8.f;
       const int xs = swz_x<CPR>(lr);
-      auto round = [&](int j, int st, int ids) {
+      auto round = [&](int j, int st) {
         const int n0 = block_at(j);
         const T* kt = wbase + (long)st * L::kStage;
         wait_vm<OPS>();
@@ -203,7 +199,7 @@ void paged_stream_kernel(PagedArgs p) {
 #pragma unroll
         for (int k = 0; k < CB / TF; ++k) load_frags_tr_swz<CPR, false>(vf[k], kt + (KIND == 0 ? L::kTile : 0), 0, k * TF * 32, lane);
         wait_lds();
-        issue(j + 2, st, ids);
+        issue(j + 2, st);
 
         const bool partly = n0 + 32 > lo;
 #pragma unroll
@@ -252,18 +248,22 @@ void paged_stream_kernel(PagedArgs p) {
               mma32(oacc[hb][cb], vf[cb / TF][cb % TF], ph[hb]);
             }
         } else {
-          const Frag<T>* v[CB];
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) v[cb] = &vf[cb / TF][cb % TF];
+          for (int hb = 0; hb < HB; ++hb) {
+            const Frag<T> seen = frag_seen(limit[hb] - n0 - 4 * h, T());
 #pragma unroll
-          for (int hb = 0; hb < HB; ++hb) add_by_limit<T, CB>(oacc[hb], v, pf[hb], &ph[hb], limit[hb], lo, keys, n0, h);
+            for (int cb = 0; cb < CB; ++cb) {
+              Frag<T> v = vf[cb / TF][cb % TF];
+              take_nonfinite<T>(v, seen, oacc[hb][cb]);
+              mma32(oacc[hb][cb], v, pf[hb]);
+              mma32(oacc[hb][cb], v, ph[hb]);
+            }
+          }
         }
       };
       for (int j = 0; j < cnt; ++j) {
-        const int after = page_at(j + 4);
-        round(j, j & 1, page);
-        page = next;
-        next = after;
+        fetch_entries(j + 4);
+        round(j, j & 1);
       }
       wait_vm<0>();                                               // tiles requested past the end still land in LDS
     }
