@@ -75,7 +75,7 @@ hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s
 hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16
 hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s);     // of its partial results, and the prefix's
 hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // bf16
-constexpr int kTileWaves = 4;          // waves of paged_tile with rows of their own
+constexpr int kTileRows = 128;         // rows of a workgroup of paged_tile
 hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s);
 
 // ---- device -----------------------------------------------------------------------------------------------------
@@ -99,11 +99,11 @@ template <typename A> __device__ __forceinline__ PagedSeq paged_seq(const A& p, 
 __device__ __forceinline__ int paged_page(int entry, int n_pages) { return (uint32_t)entry < (uint32_t)n_pages ? entry : 0; }
 
 // Which sequence item `target` belongs to when every sequence has items(b) of them, one behind the other: its number (-1: behind
-// the last), the item's index in it, and the number of all items.  All NT threads call; `sh` holds NT / 64 + 2 words.
-template <int NT = 256, class F>
+// the last), the item's index in it, and the number of all items.  All 256 threads call; `sh` holds 6 words.
+template <class F>
 __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh, int& index, int& total) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int per = (B + NT - 1) / NT, first = tid * per, last = min(B, first + per);
+  const int per = (B + 255) / 256, first = tid * per, last = min(B, first + per);
   int mine = 0;
   for (int b = first; b < last; ++b) mine += items(b);
   int x = mine;
@@ -112,7 +112,7 @@ __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh,
     const int y = __shfl_up(x, d);
     if (lane >= d) x += y;
   }
-  constexpr int W = NT / kWave;
+  constexpr int W = 256 / kWave;
   if (lane == kWave - 1) sh[wave] = x;
   if (tid == 0) sh[W] = -1;
   __syncthreads();

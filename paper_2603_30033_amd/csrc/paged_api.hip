@@ -24,7 +24,11 @@ int check_pool(const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucke
   const tucker_attn_config& f = c->cfg;
   if (f.shared_kv ? p->V != nullptr : p->V == nullptr) return TUCKER_ATTN_INVALID_ARG;
   if (!aligned16(p->K) || !aligned16(p->V)) return TUCKER_ATTN_INVALID_ARG;
-  auto stride_ok = [&](int64_t s, int r) { return s == 0 || (s >= (int64_t)p->page_size * r && (s * c->es) % 16 == 0); };
+  // (strides are counted in 16-byte units of 32 bits)
+  auto stride_ok = [&](int64_t s, int r) {
+    const int64_t least = (int64_t)p->page_size * r;
+    return (s == 0 || (s >= least && (s * c->es) % 16 == 0)) && (s == 0 ? least : s) <= 0xffffffffl * 4;
+  };
   if (!stride_ok(p->k_stride, f.r3) || (!f.shared_kv && !stride_ok(p->v_stride, f.rt3))) return TUCKER_ATTN_INVALID_ARG;
   if (!b->q_start || !b->kv_len || !b->page_table) return TUCKER_ATTN_INVALID_ARG;
   if (b->max_len > (long)b->max_pages * p->page_size) return TUCKER_ATTN_INVALID_ARG;
@@ -61,7 +65,7 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const int keys = b->max_len - prefix;
   a.hb = f.dtype != TUCKER_ATTN_BF16 ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
   const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // paged_tile: fp32 rows go through paged_rows
-  const int block = tile ? 32 * kTileWaves : 32, wgs = tile ? 1 : 2, least = tile ? 256 : 128;
+  const int block = tile ? kTileRows : 32, wgs = 2, least = tile ? 256 : 128;
   a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, wgs, least) : 0;
   a.stream_wgs = 0;
   if (a.hb > 0) {
