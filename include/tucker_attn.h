@@ -293,7 +293,7 @@ typedef struct {
  *            already), and Q must be NULL.  Without latent RoPE nothing is rotated
  * A token before its sequence's first row (kv_len too small) is not stored.  Two tokens that name the same row are a race.
  * Any alignment of K, V, Q, Qrot and of ldk, ldv; rows that start on 16 bytes are read and written whole.
- * UNSUPPORTED_SHAPE: pool rows that are no multiple of 16 bytes; T * n_heads of 2^31 and more.
+ * UNSUPPORTED_SHAPE: pool rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more.
  */
 int tucker_attn_append_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
                              const void *K, int64_t ldk, const void *V, int64_t ldv, const void *Q, void *Qrot,
@@ -314,7 +314,7 @@ size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tuck
  *   O    device [T, n_heads, rt3]  out, storage type
  *   lse  device [T, n_heads] fp32  out, natural logarithm; may be NULL
  * One new token per sequence (decode), a few (proposed tokens) or many (pieces of a prompt).  Q and O start on 16 bytes.
- * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; T * n_heads of 2^31 and more.
+ * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more.
  */
 int tucker_attn_attend_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
                              const void *Q, void *O, float *lse, void *workspace, size_t workspace_bytes,

@@ -44,9 +44,11 @@ struct PagedArgs {
   float2* part_ml;              // [parts][T * nH]
   int prefix_parts;             // parts 0 .. prefix_parts-1: the prefix
   int own_parts;                // then those of the sequence's own rows; 0: written to O directly
-  // few rows a sequence (paged_stream): 32-row blocks of a sequence, workgroups that share all sequences' keys (0: one for every
-  // sequence), and partial results of sequences that several share, [2 * stream_wgs][hb * 32] rows
-  int hb, stream_wgs;
+  int prefix_keys, own_keys;    // keys of such parts (a short sequence leaves the last parts empty: no output, a sum of 0)
+  // The keys of all sequences dealt to workgroups in equal shares (0: a workgroup for every sequence, or row block): of paged_stream,
+  // which takes a sequence's `hb` blocks of 32 rows at once, and of paged_tile.  Rows that several workgroups share leave partial
+  // results, [2 * workgroups][hb * 32 or kTileRows] rows.
+  int hb, stream_wgs, tile_wgs;
   float* stream_o;
   float2* stream_ml;
 };
@@ -75,8 +77,9 @@ hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s
 hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16
 hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s);     // of its partial results, and the prefix's
 hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // bf16
-constexpr int kTileRows = 128;         // rows of a workgroup of paged_tile
-hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s);
+constexpr int kTileRows = 128, kTileUnit = 64, kTileLeast = 4;   // rows of a workgroup of paged_tile, keys of a unit of its work, least units
+hipError_t launch_paged_tile_join(const PagedArgs& a, hipStream_t s);
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s);   // fp32
 
 // ---- device -----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ int divide(int n, Divisor d) { return (int)(__umulhi((uint32_t)n * 2u, d.mul) >> d.shift); }
@@ -135,6 +138,21 @@ __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh,
   __syncthreads();
   return found;
 }
+
+// `units` units of work in equal shares for at most `wgs` workgroups, at least `least` units each (the first units % G have one more)
+struct Shares {
+  int n, more, G;
+  __device__ __forceinline__ Shares(int units, int wgs, int least) {
+    G = max(1, min(wgs, (units + least - 1) / least));
+    n = units / G;
+    more = units % G;
+  }
+  __device__ __forceinline__ int first(int g) const { return g * n + min(g, more); }         // unit of workgroup g
+  __device__ __forceinline__ int group(int u) const {                                        // workgroup of unit u
+    const int m = more * (n + 1);
+    return u < m ? u / (n + 1) : more + (u - m) / n;
+  }
+};
 
 // four output channels c .. c+3 of one row
 template <typename T>

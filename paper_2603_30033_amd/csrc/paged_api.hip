@@ -24,12 +24,11 @@ int check_pool(const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucke
   const tucker_attn_config& f = c->cfg;
   if (f.shared_kv ? p->V != nullptr : p->V == nullptr) return TUCKER_ATTN_INVALID_ARG;
   if (!aligned16(p->K) || !aligned16(p->V)) return TUCKER_ATTN_INVALID_ARG;
-  // (strides are counted in 16-byte units of 32 bits)
-  auto stride_ok = [&](int64_t s, int r) {
-    const int64_t least = (int64_t)p->page_size * r;
-    return (s == 0 || (s >= least && (s * c->es) % 16 == 0)) && (s == 0 ? least : s) <= 0xffffffffl * 4;
-  };
+  auto stride_ok = [&](int64_t s, int r) { return s == 0 || (s >= (int64_t)p->page_size * r && (s * c->es) % 16 == 0); };
   if (!stride_ok(p->k_stride, f.r3) || (!f.shared_kv && !stride_ok(p->v_stride, f.rt3))) return TUCKER_ATTN_INVALID_ARG;
+  // (the kernels count 16-byte units of a pool in 32 bits)
+  auto small = [&](int64_t s, int r) { return (double)p->n_pages * (s ? s : (double)p->page_size * r) * c->es < 16.0 * 0xffffffffu; };
+  if (!small(p->k_stride, f.r3) || (!f.shared_kv && !small(p->v_stride, f.rt3))) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   if (!b->q_start || !b->kv_len || !b->page_table) return TUCKER_ATTN_INVALID_ARG;
   if (b->max_len > (long)b->max_pages * p->page_size) return TUCKER_ATTN_INVALID_ARG;
   return TUCKER_ATTN_OK;
@@ -54,6 +53,9 @@ int key_parts(const tucker_attn_ctx* c, long blocks, int keys, int wgs, int leas
   return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
+// Keys of each of these parts: whole tiles
+int part_keys(int keys, int parts) { return keys < 1 ? 64 : ((keys + parts - 1) / parts + 63) / 64 * 64; }
+
 // Longest keys that one workgroup takes alone rather than several and a second launch that joins their results
 constexpr int kStreamWhole = 512;
 
@@ -65,17 +67,25 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const int keys = b->max_len - prefix;
   a.hb = f.dtype != TUCKER_ATTN_BF16 ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
   const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // paged_tile: fp32 rows go through paged_rows
-  const int block = tile ? kTileRows : 32, wgs = 2, least = tile ? 256 : 128;
-  a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, wgs, least) : 0;
-  a.stream_wgs = 0;
+  const int block = tile ? kTileRows : 32;
+  a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, tile ? 1 : 2, tile ? 256 : 128) : 0;
+  a.prefix_keys = a.prefix_parts > 0 ? part_keys(prefix, a.prefix_parts) : 0;
+  a.stream_wgs = a.tile_wgs = 0;
+  a.own_parts = prefix > 0 ? 1 : 0;                               // rows that one workgroup does alone
+  long shared = 0;                                                // rows of partial results that workgroups share
   if (a.hb > 0) {
-    a.own_parts = prefix > 0 ? 1 : 0;                             // sequences that one workgroup does alone
     if (keys > kStreamWhole) a.stream_wgs = c->n_cus;
+    shared = 2l * a.stream_wgs * a.hb * 32;
+  } else if (tile) {
+    const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
+    if (units > kTileLeast && blocks * units < (1l << 31)) a.tile_wgs = 2 * c->n_cus;
+    shared = 2l * a.tile_wgs * kTileRows;
   } else {
-    a.own_parts = key_parts(c, paged_rows_blocks(a, block), keys, wgs, least);
-    if (a.own_parts == 1 && prefix == 0) a.own_parts = 0;
+    const int parts = key_parts(c, paged_rows_blocks(a, block), keys, 2, 128);
+    a.own_keys = part_keys(keys, parts);
+    if (parts > 1) a.own_parts = parts;
   }
-  const size_t parts = a.prefix_parts + a.own_parts, shared = 2ul * a.stream_wgs * a.hb * 32;
+  const size_t parts = a.prefix_parts + a.own_parts;
   Carver cv{static_cast<char*>(ws), 0};
   a.part_o = cv.take<float>(parts * rows * c->D * 4);
   a.part_ml = cv.take<float2>(parts * rows * 8);
@@ -113,8 +123,9 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
   if ((a.hb > 0 ? launch_paged_stream(a, s) : tile ? launch_paged_tile(a, false, s) : launch_paged_rows(a, false, s)) != hipSuccess)
     return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("paged_attention");
-  if (a.prefix_parts + a.own_parts + a.stream_wgs > 0) {
-    if ((a.hb > 0 ? launch_paged_join(a, s) : launch_paged_merge(f.dtype, a, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (a.prefix_parts + a.own_parts + a.stream_wgs + a.tile_wgs > 0) {
+    if ((a.hb > 0 ? launch_paged_join(a, s) : tile ? launch_paged_tile_join(a, s) : launch_paged_merge(a, s)) != hipSuccess)
+      return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("paged_merge");
   }
   return TUCKER_ATTN_OK;

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
   const int hi = causal ? len - nq + divide(min(rb * 32 + 31, n_rows - 1), p.heads) + 1 : len;
   const int lo = causal ? len - nq + divide(rb * 32, p.heads) + 1 : len;       // keys that all rows of the block see
   const int blocks = hi > first ? (hi - first + 31) / 32 : 0;
-  const int per = (blocks + parts - 1) / parts;
+  const int per = (PREFIX ? p.prefix_keys : p.own_keys) / 32;
   const int k0 = part * per, k1 = min(blocks, k0 + per);
 
   Frag<T> qf[CB];
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
                           : static_cast<const T*>(p.V) + pg * p.v_stride + off * p.rt3;
         frag_set(vf, e, to_f32(src[c]));
       }
-      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) take_nonfinite<T>(vf, frag_seen(limit - n0 - 4 * h, T()), oacc[cb]);
+      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) take_nonfinite<T>(vf, limit - n0 - 4 * h, oacc[cb]);
       mma32(oacc[cb], vf, pf);
       if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
     }
@@ -141,28 +141,25 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// partial results of a row joined: one row by D/4 threads
+// partial results of a row joined: a row by D/4 threads, or by `groups` times as many that take every groups-th part
 // ------------------------------------------------------------------------------------------------------------------
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p) {
-  constexpr int L = D / 4;
-  const long rows = (long)p.T * p.nH, row = (long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int c = threadIdx.x % L * 4;
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p, int groups) {
+  constexpr int L = D / 4, SLOTS = 256 / L;
+  __shared__ float4 po[256];
+  __shared__ float2 pml[SLOTS];
+  const int tid = threadIdx.x, slot = tid / L, c = tid % L * 4, per = SLOTS / groups, group = slot / per;
+  const long rows = (long)p.T * p.nH, row = (long)blockIdx.x * per + slot % per;
   const int q0 = min(max(p.q_start[0], 0), p.T), q1 = min(max(p.q_start[p.B], 0), p.T);
-  if (row < (long)q0 * p.nH || row >= (long)q1 * p.nH) return;    // behind the last sequence
-  const int parts = p.prefix_parts + p.own_parts;
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < parts; ++i) {
-    const float2 ml = p.part_ml[i * rows + row];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_o + (i * rows + row) * D + c);
-    if (ml.x == -INFINITY) continue;
-    const float m_new = fmaxf(m, ml.x), a = fast_exp2(m - m_new), b = fast_exp2(ml.x - m_new);
-    m = m_new;
-    l = l * a + ml.y * b;
-    o = o * a + v * b;
-  }
-  paged_result<T>(p, row, c, m, l, o);
+  const bool live = row >= (long)q0 * p.nH && row < (long)q1 * p.nH;   // not behind the last sequence
+  RowSum sum;
+  if (live)
+    sum.add_parts(p.prefix_parts + p.own_parts, group, groups, [&](int i, const float2*& ml, const float*& o) {
+      ml = p.part_ml + i * rows + row;
+      o = p.part_o + (i * rows + row) * D + c;
+    });
+  sum.add_groups(po, pml, slot, group, groups, per, L);
+  if (group == 0 && live) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -196,17 +193,17 @@ hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s
 
 template <typename T> static hipError_t merge_dispatch(const PagedArgs& a, hipStream_t s) {
   const long rows = (long)a.T * a.nH;
-  auto grid = [&](int per) { return dim3((uint32_t)((rows + per - 1) / per)); };
+  int groups = 1;                                                 // 8 parts a thread
+  while (groups < 8 && 8 * groups < a.prefix_parts + a.own_parts) groups *= 2;
+  auto grid = [&](int slots) { return dim3((uint32_t)((rows + slots / groups - 1) / (slots / groups))); };
   switch (a.D) {
-    case 32: hipLaunchKernelGGL((paged_merge_kernel<T, 32>), grid(32), dim3(256), 0, s, a); break;
-    case 64: hipLaunchKernelGGL((paged_merge_kernel<T, 64>), grid(16), dim3(256), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((paged_merge_kernel<T, 128>), grid(8), dim3(256), 0, s, a); break;
+    case 32: hipLaunchKernelGGL((paged_merge_kernel<T, 32>), grid(32), dim3(256), 0, s, a, groups); break;
+    case 64: hipLaunchKernelGGL((paged_merge_kernel<T, 64>), grid(16), dim3(256), 0, s, a, groups); break;
+    case 128: hipLaunchKernelGGL((paged_merge_kernel<T, 128>), grid(8), dim3(256), 0, s, a, groups); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
-hipError_t launch_paged_merge(int dtype, const PagedArgs& a, hipStream_t s) {
-  return dtype == 0 ? merge_dispatch<float>(a, s) : merge_dispatch<bf16>(a, s);
-}
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s) { return merge_dispatch<float>(a, s); }
 
 }  // namespace ta

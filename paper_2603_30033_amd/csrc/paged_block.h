@@ -8,10 +8,13 @@ namespace ta {
 // 16 channels c0 .. of a row of r channels (whole 16-byte chunks), zeros behind them
 template <typename T> __device__ __forceinline__ Frag<T> load_frag_upto(const T* row, int c0, int r) {
   constexpr int CE = 16 / (int)sizeof(T), NC = 16 / CE;
-  Frag<T> f = zero_frag<T>();
+  Frag<T> f;
 #pragma unroll
-  for (int i = 0; i < NC; ++i)
-    if (c0 + i * CE < r) f.v[i] = *reinterpret_cast<const decltype(f.v[0] + f.v[0])*>(row + c0 + i * CE);
+  for (int i = 0; i < NC; ++i) {                                  // (no branches: the loads go together)
+    const int c = c0 + i * CE;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(row + (c < r ? c : 0));
+    f.v[i] = __builtin_bit_cast(__typeof__(f.v[0] + f.v[0]), c < r ? x : u32x4{0u, 0u, 0u, 0u});
+  }
   return f;
 }
 
@@ -71,56 +74,46 @@ template <typename T> __device__ __forceinline__ bool frag_finite(const Frag<T>&
   }
   return (any & Bits<T>::kTop) == 0;
 }
-// 1 for the keys of a block that the row sees: `live` of them, as this lane counts (minus 4h)
-__device__ __forceinline__ Frag<bf16> frag_seen(int live, bf16) {
-  Frag<bf16> f;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    u32x4 w;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {                                 // elements 8i + 2d, + 1: keys 8 (e / 4) + e % 4 (+ 4h)
-      const int key = 16 * i + 8 * (d / 2) + 2 * (d % 2);
-      w[d] = ((uint32_t)((key - live) >> 31) & 0x3f80u) | ((uint32_t)((key + 1 - live) >> 31) & 0x3f800000u);
-    }
-    f.v[i] = __builtin_bit_cast(bf16x8, w);
+// element pair (element) d of part i of a fragment for the keys of a block that the row sees -- `live` of them, as this lane counts
+// (minus 4h) -- : ones, else zeros
+template <typename T> __device__ __forceinline__ uint32_t seen_word(int i, int d, int live) {
+  if constexpr (sizeof(T) == 2) {                                 // elements 8i + 2d, + 1: keys 8 (e / 4) + e % 4 (+ 4h)
+    const int key = 16 * i + 8 * (d / 2) + 2 * (d % 2);
+    return ((uint32_t)((key - live) >> 31) & 0x3f80u) | ((uint32_t)((key + 1 - live) >> 31) & 0x3f800000u);
+  } else {
+    return (uint32_t)((8 * i + d - live) >> 31) & 0x3f800000u;
   }
-  return f;
 }
-__device__ __forceinline__ Frag<float> frag_seen(int live, float) {
-  Frag<float> f;
+__device__ __forceinline__ void mma_part(f32x16& n, const bf16x8& a, const bf16x8& b) { n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, n, 0, 0, 0); }
+__device__ __forceinline__ void mma_part(f32x16& n, const f32x4& a, const f32x4& b) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    u32x4 w;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) w[d] = (uint32_t)((8 * i + d - live) >> 31) & 0x3f800000u;
-    f.v[i] = __builtin_bit_cast(f32x4, w);
-  }
-  return f;
+  for (int j = 0; j < 4; ++j) n = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], n, 0, 0, 0);
 }
 // v without its elements that are not finite, which go to the sums o of its 32 channels and of the rows that see their key
-template <typename T> __device__ __forceinline__ void take_nonfinite(Frag<T>& v, const Frag<T>& seen, f32x16& o) {
+template <typename T> __device__ __forceinline__ void take_nonfinite(Frag<T>& v, int live, f32x16& o) {
   using B = Bits<T>;
-  __builtin_amdgcn_sched_barrier(0);                              // (one fragment at a time: few registers)
-  Frag<T> stand;
+  using Part = __typeof__(v.v[0] + v.v[0]);
+  f32x16 n;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) n[e] = 0.f;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(Frag<T>) / 16; ++i) {
-    u32x4 w = __builtin_bit_cast(u32x4, v.v[i]), x;
+    __builtin_amdgcn_sched_barrier(0);                            // (one part at a time: few registers)
+    u32x4 w = __builtin_bit_cast(u32x4, v.v[i]), x, y;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       const uint32_t bad = (((w[d] & B::kExp) + B::kLow) >> B::kSign) & B::kUnit;
       const uint32_t nan = (((w[d] & B::kMant) + B::kMant) >> B::kMantBits) & bad, minus = (w[d] >> B::kSign) & bad & ~nan;
       x[d] = nan * B::kNan + minus * B::kMinus + (bad & ~nan & ~minus) * B::kPlus;
       w[d] &= ~(bad * B::kAll);
+      y[d] = seen_word<T>(i, d, live);
     }
-    v.v[i] = __builtin_bit_cast(__typeof__(v.v[0] + v.v[0]), w);
-    stand.v[i] = __builtin_bit_cast(__typeof__(v.v[0] + v.v[0]), x);
+    v.v[i] = __builtin_bit_cast(Part, w);
+    mma_part(n, __builtin_bit_cast(Part, x), __builtin_bit_cast(Part, y));   // up to 32 of each kind: exact
   }
-  f32x16 n;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) n[e] = 0.f;
-  mma32(n, stand, seen);                                          // up to 32 of each kind: exact
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
+    if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
     o[e] += n[e] >= 1.f ? INFINITY : 0.f;
     o[e] += __builtin_amdgcn_fractf(n[e]) > 0.f ? -INFINITY : 0.f;
     o[e] += n[e] >= 1024.f ? NAN : 0.f;
@@ -199,5 +192,64 @@ template <int D> __device__ __forceinline__ void paged_partial(float* po, float2
   *reinterpret_cast<f32x4*>(po + slot * D + c) = o;
   if (c == 0) pml[slot] = float2{m, l};
 }
+
+// Partial results of one row, four channels a thread: (m, l, o) with sum and output relative to 2^m
+struct RowSum {
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float2 ml, f32x4 v, bool live = true) {
+    live = live && ml.x != -INFINITY;                             // (an empty part's output may never have been written)
+    const float top = fmaxf(m, live ? ml.x : -INFINITY), ref = top == -INFINITY ? 0.f : top;
+    const float a = fast_exp2(m - ref), f = live ? fast_exp2(ml.x - ref) : 0.f;
+    m = top;
+    l = l * a + (live ? ml.y * f : 0.f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * a + (live ? v[e] * f : 0.f);
+  }
+  // U of the parts base + group, + groups, ..; where(i, ml, o): where part i is.  The loads are in flight together.
+  template <int U, class W> __device__ __forceinline__ void add_batch(int base, int parts, int group, int groups, W where) {
+    float2 ml[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float2* pm;
+      const float* po;
+      where(min(base + group + k * groups, parts - 1), pm, po);
+      ml[k] = *pm;
+      v[k] = *reinterpret_cast<const f32x4*>(po);
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) add(ml[k], v[k], base + group + k * groups < parts);
+  }
+  // parts group, group + groups, ..
+  template <class W> __device__ __forceinline__ void add_parts(int parts, int group, int groups, W where) {
+    for (int base = 0; base < parts;) {
+      const int left = parts - base;
+      if (left > 4 * groups) {
+        add_batch<8>(base, parts, group, groups, where);
+        base += 8 * groups;
+      } else if (left > 2 * groups) {
+        add_batch<4>(base, parts, group, groups, where);
+        base += 4 * groups;
+      } else {
+        add_batch<2>(base, parts, group, groups, where);
+        base += 2 * groups;
+      }
+    }
+  }
+  // the sums of a row's other groups of threads, in their order, into group 0's.  po [256], pml [256 / L]; all threads call.
+  __device__ __forceinline__ void add_groups(float4* po, float2* pml, int slot, int group, int groups, int per, int L) {
+    if (groups == 1) return;
+    const int tid = threadIdx.x;
+    po[tid] = float4{o[0], o[1], o[2], o[3]};
+    if (tid % L == 0) pml[slot] = float2{m, l};
+    __syncthreads();
+    if (group > 0) return;
+    for (int k = 1; k < groups; ++k) {
+      const float4 v = po[tid + k * per * L];
+      add(pml[slot + k * per], f32x4{v.x, v.y, v.z, v.w});
+    }
+  }
+};
 
 }  // namespace ta

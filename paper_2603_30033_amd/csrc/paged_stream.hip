@@ -29,15 +29,8 @@ template <int D, int KIND> struct StreamLds {
 // units of sequence b (no new token: none; no key of its own: one, which leaves its rows' empty result)
 __device__ __forceinline__ int stream_units(const PagedArgs& p, int b) {
   const PagedSeq s = paged_seq(p, b);
-  return s.nq == 0 ? 0 : max(1, (s.len - p.prefix + kUnit - 1) / kUnit);
+  return (int)(s.nq != 0) * max(1, (s.len - p.prefix + kUnit - 1) / kUnit);   // (no branch: the loads go together)
 }
-// shares: first unit of workgroup g of G, and the workgroup of unit u; at least kStreamLeast units each
-__device__ __forceinline__ int stream_groups(const PagedArgs& p, int units) {
-  return max(1, min(p.stream_wgs, (units + kStreamLeast - 1) / kStreamLeast));
-}
-__device__ __forceinline__ int stream_first(int g, int units, int G) { return (int)((long)g * units / G); }
-__device__ __forceinline__ int stream_group(int u, int units, int G) { return (int)(((long)(u + 1) * G - 1) / units); }
-
 template <int D, int HB, int KIND>
 // (wide latents: LDS leaves one wave to a SIMD, which may then use all registers)
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, HB == 1 && D < 128 ? 2 : 1)))
@@ -60,10 +53,10 @@ void paged_stream_kernel(PagedArgs p) {
     int units;
     b = paged_locate(p.B, 0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
     if (b < 0) return;
-    const int G = stream_groups(p, units), g = blockIdx.x;
-    if (g >= G) return;
-    const int u0 = stream_first(g, units, G);
-    left = stream_first(g + 1, units, G) - u0;
+    const Shares sh(units, p.stream_wgs, kStreamLeast);
+    if ((int)blockIdx.x >= sh.G) return;
+    const int u0 = sh.first(blockIdx.x);
+    left = sh.first(blockIdx.x + 1) - u0;
     if (u0 > 0) b = paged_locate(p.B, u0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
   }
   if (left == 0) return;
@@ -96,6 +89,13 @@ void paged_stream_kernel(PagedArgs p) {
     }
 
     if (unit0 < keys) {                                           // (the same for the whole workgroup)
+      // 16 rows in one page that fill the tile's width: one start for the wave, and what its lanes add to it (in bytes, of the first
+      // piece; the others' differ in two bits of the chunk and in the row).  Rows behind the sequence's last are whatever the page
+      // holds.  Else every lane looks up its own row.
+      constexpr int PPG = 16 / RPP;
+      static_assert(PPG == 1 || swz_x<CPR>(RPP) == 4, "four chunks a piece");
+      const bool straight = p.page_size % 16 == 0 && p.prefix % 16 == 0 && p.r3 == D && (KIND != 0 || p.rt3 == D);
+      const uint32_t add0 = lane / CPR * (D * 2) + ((lane % CPR) ^ swz_x<CPR>(lane / CPR)) * 16;
       auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
       // The table entries of block j's rows come by way of LDS too: an entry in a register would be waited for with every tile
       // behind it.  Rows behind the last repeat it and are masked.
@@ -107,18 +107,32 @@ void paged_stream_kernel(PagedArgs p) {
         const int n0 = block_at(j);
         const int* ids = entries + (j & 3) * 64;
         T* kt = wbase + (long)st * L::kStage;
-        int l = lane;
-        asm volatile("" : "+v"(l));                               // (rows and chunks of the pieces are formed afresh, not kept across the loop)
+        if (straight) {
+          const char *k = nullptr, *v = nullptr;
 #pragma unroll
-        for (int q = 0; q < PIECES; ++q) {
-          const int row = q * RPP + l / CPR, c = ((l % CPR) ^ swz_x<CPR>(row)) * 8;
-          const int n = min(n0 + row, keys - 1);
-          const long pg = paged_page(ids[row], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
-          const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3 + c;
-          chunk_to_lds(c < p.r3 ? kp : reinterpret_cast<const T*>(paged_zeros), kt + q * 512);
-          if constexpr (KIND == 0) {
-            const T* vp = static_cast<const T*>(p.V) + pg * p.v_stride + a * p.rt3 + c;
-            chunk_to_lds(c < p.rt3 ? vp : reinterpret_cast<const T*>(paged_zeros), kt + L::kTile + q * 512);
+          for (int q = 0; q < PIECES; ++q) {
+            if (q % PPG == 0) {                                   // the next 16 rows: they lie in one page
+              const int row = q * RPP, n = n0 + row;
+              const long pg = paged_page(__builtin_amdgcn_readfirstlane(ids[row]), p.n_pages), a = n - divide(n, p.ps) * p.page_size;
+              k = static_cast<const char*>(p.K) + (pg * p.k_stride + a * D) * 2;
+              if constexpr (KIND == 0) v = static_cast<const char*>(p.V) + (pg * p.v_stride + a * D) * 2;
+            }
+            const uint32_t add = (add0 ^ (64 * (q % PPG))) + q % PPG * 1024;
+            chunk_to_lds(k + add, kt + q * 512);
+            if constexpr (KIND == 0) chunk_to_lds(v + add, kt + L::kTile + q * 512);
+          }
+        } else {
+#pragma unroll 1
+          for (int q = 0; q < PIECES; ++q) {
+            const int row = q * RPP + lane / CPR, c = ((lane % CPR) ^ swz_x<CPR>(row)) * 8;
+            const int n = min(n0 + row, keys - 1);
+            const long pg = paged_page(ids[row], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
+            const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3 + c;
+            chunk_to_lds(c < p.r3 ? kp : reinterpret_cast<const T*>(paged_zeros), kt + q * 512);
+            if constexpr (KIND == 0) {
+              const T* vp = static_cast<const T*>(p.V) + pg * p.v_stride + a * p.rt3 + c;
+              chunk_to_lds(c < p.rt3 ? vp : reinterpret_cast<const T*>(paged_zeros), kt + L::kTile + q * 512);
+            }
           }
         }
         if constexpr (ROT) {
@@ -250,11 +264,10 @@ void paged_stream_kernel(PagedArgs p) {
         } else {
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb) {
-            const Frag<T> seen = frag_seen(limit[hb] - n0 - 4 * h, T());
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
               Frag<T> v = vf[cb / TF][cb % TF];
-              take_nonfinite<T>(v, seen, oacc[hb][cb]);
+              take_nonfinite<T>(v, limit[hb] - n0 - 4 * h, oacc[hb][cb]);
               mma32(oacc[hb][cb], v, pf[hb]);
               mma32(oacc[hb][cb], v, ph[hb]);
             }
@@ -303,7 +316,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups
   const int n_rows = s.nq * p.nH, per = SLOTS / groups;
   if ((int)blockIdx.y * per >= n_rows) return;
 
-  int g0 = 0, g1 = 0, u0 = 0, units = 0, G = 1;                   // workgroups that share the sequence
+  int g0 = 0, g1 = 0;                                             // workgroups that share the sequence,
+  bool cut = false;                                               // the first of them behind another sequence
   if (p.stream_wgs > 0) {
     int before = 0, all = 0;
     for (int i = tid; i < p.B; i += 256) {
@@ -321,58 +335,31 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups
       sums[4 + tid / kWave] = before;
     }
     __syncthreads();
-    units = sums[0] + sums[1] + sums[2] + sums[3];
-    u0 = sums[4] + sums[5] + sums[6] + sums[7];
-    G = stream_groups(p, units);
-    g0 = stream_group(u0, units, G);
-    g1 = stream_group(u0 + stream_units(p, b) - 1, units, G);
+    const int units = sums[0] + sums[1] + sums[2] + sums[3], u0 = sums[4] + sums[5] + sums[6] + sums[7];
+    const Shares sh(units, p.stream_wgs, kStreamLeast);
+    g0 = sh.group(u0);
+    g1 = sh.group(u0 + stream_units(p, b) - 1);
+    cut = sh.first(g0) < u0;
   }
   const bool complete = g0 == g1;                                 // one workgroup did it all
   if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
-  const int parts = p.prefix_parts + (g1 - g0 + 1);
   const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
   const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + r;
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  RowSum sum;
   if (r < n_rows) {
-    constexpr int U = 8;                                          // parts whose loads are in flight together
-    for (int i0 = group; i0 < parts; i0 += U * groups) {
-      float2 ml[U];
-      f32x4 v[U];
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int i = min(i0 + k * groups, parts - 1), g = g0 + i - p.prefix_parts;
-        const bool by_row = i < p.prefix_parts || complete;
-        const long at = by_row ? i * rows + row : (2l * g + (stream_first(g, units, G) < u0)) * (p.hb * 32) + r;
-        ml[k] = (by_row ? p.part_ml : p.stream_ml)[at];
-        v[k] = *reinterpret_cast<const f32x4*>((by_row ? p.part_o : p.stream_o) + at * D + c);
-      }
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        if (i0 + k * groups >= parts || ml[k].x == -INFINITY) continue;
-        const float top = fmaxf(m, ml[k].x), a = fast_exp2(m - top), f = fast_exp2(ml[k].x - top);
-        m = top;
-        l = l * a + ml[k].y * f;
-        o = o * a + v[k] * f;
-      }
-    }
+    sum.add_parts(p.prefix_parts + (complete ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
+      ml = p.part_ml + i * rows + row;
+      o = p.part_o + (i * rows + row) * D + c;
+    });
+    if (!complete)
+      sum.add_parts(g1 - g0 + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
+        const long at = (2l * (g0 + i) + (cut && i == 0)) * (p.hb * 32) + r;
+        ml = p.stream_ml + at;
+        o = p.stream_o + at * D + c;
+      });
   }
-  if (groups > 1) {                                               // the groups' sums, in their order
-    po[tid] = float4{o[0], o[1], o[2], o[3]};
-    if (c == 0) pml[slot] = float2{m, l};
-    __syncthreads();
-    if (group > 0) return;
-    for (int k = 1; k < groups; ++k) {
-      const float2 ml = pml[slot + k * per];
-      if (ml.x == -INFINITY) continue;
-      const float4 v = po[tid + k * per * L];
-      const float top = fmaxf(m, ml.x), a = fast_exp2(m - top), f = fast_exp2(ml.x - top);
-      m = top;
-      l = l * a + ml.y * f;
-      o = o * a + f32x4{v.x, v.y, v.z, v.w} * f;
-    }
-  }
-  if (r < n_rows) paged_result<T>(p, row, c, m, l, o);
+  sum.add_groups(po, pml, slot, group, groups, per, L);
+  if (group == 0 && r < n_rows) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -401,10 +388,10 @@ hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s) {
 
 template <int D> static hipError_t join_one(const PagedArgs& a, hipStream_t s) {
   constexpr int SLOTS = 256 / (D / 4);
-  // parts that a sequence has on average: that many groups of threads share a row's
+  // one group of threads for every 8 parts that a sequence has on average
   const int parts = a.prefix_parts + (a.stream_wgs > 0 ? a.stream_wgs / a.B : 0) + 1;
   int groups = 1;
-  while (groups < 8 && 4 * groups < parts) groups *= 2;
+  while (groups < 8 && 8 * groups < parts) groups *= 2;
   const int per = SLOTS / groups, most = a.max_new * a.nH;
   hipLaunchKernelGGL(paged_join_kernel<D>, dim3(a.B, (most + per - 1) / per), dim3(256), 0, s, a, groups);
   return hipGetLastError();

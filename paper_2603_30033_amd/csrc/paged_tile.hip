@@ -10,8 +10,6 @@
 // result is: the relative error of the sum is that of one more rounding of the result.
 #include "paged_block.h"
 
-#include <type_traits>
-
 namespace ta {
 
 // KIND 0: key and value pools; 1: one pool, keys rotated on their way into LDS, kept as two bf16 parts; 2: one pool, nothing rotated
@@ -24,6 +22,11 @@ template <int D, int KIND> struct TileLds {
   static constexpr size_t kBytes = kTiles + kEntries;
 };
 
+// row blocks of sequence b, and units of keys of each of them (no key of its own: one, which leaves the rows' empty result).  Rows that
+// see fewer keys than the sequence has count alike.
+__device__ __forceinline__ int tile_blocks(const PagedArgs& p, int b) { return (paged_seq(p, b).nq * p.nH + kTileRows - 1) / kTileRows; }
+__device__ __forceinline__ int tile_units(const PagedArgs& p, int b) { return max(1, (paged_seq(p, b).len - p.prefix + kTileUnit - 1) / kTileUnit); }
+
 template <int D, int KIND, bool PREFIX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tile_kernel(PagedArgs p) {
   using T = bf16;
@@ -34,46 +37,67 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   T* smem = reinterpret_cast<T*>(smem_raw);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, lr = lane % 32;
-  const int parts = PREFIX ? p.prefix_parts : max(p.own_parts, 1), part = blockIdx.y;
 
   // ---- which rows, which keys ----
-  int rb, n_rows, row0;                                           // block, rows of its sequence, first row of that in [T * nH]
-  int first, len, nq, pages;
-  const int* table;
+  // Workgroups go to the eight dies in turn, and each die has a cache of its own: workgroup i of a die takes piece i of the die's
+  // share of consecutive pieces, which read the same keys.
+  const int die = blockIdx.x % 8, in_die = blockIdx.x / 8;
+  int b = 0, rb, unit = 0, left = 1, units_b = 1, part = 0, me = 0;   // sequence, row block, unit of its keys, units to do, units of a block
   if constexpr (PREFIX) {
-    rb = blockIdx.x;
-    row0 = 0;
-    nq = min(max(p.q_start[p.B], 0), p.T);
-    n_rows = nq * p.nH;
-    first = 0;
-    len = p.prefix;
-    table = p.prefix_table;
-    pages = divide(p.prefix - 1, p.ps) + 1;
-    if (rb * RB >= n_rows) return;
+    const int blocks = (p.T * p.nH + RB - 1) / RB, per = (blocks * p.prefix_parts + 7) / 8, piece = die * per + in_die;
+    if (in_die >= per || piece >= blocks * p.prefix_parts) return;
+    part = piece / blocks;
+    rb = piece % blocks;
   } else {
-    int total;
-    const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return (paged_seq(p, i).nq * p.nH + RB - 1) / RB; },
-                               reinterpret_cast<int*>(smem_raw), rb, total);
-    if (b < 0) return;
+    int index, units;
+    if (p.tile_wgs == 0) {                                        // a workgroup for every row block
+      b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, i); }, reinterpret_cast<int*>(smem_raw), rb, units);
+      if (b < 0) return;
+      left = units_b = tile_units(p, b);
+    } else {
+      auto all = [&](int i) { return tile_blocks(p, i) * tile_units(p, i); };
+      b = paged_locate(p.B, 0, all, reinterpret_cast<int*>(smem_raw), index, units);
+      if (b < 0) return;
+      const Shares sh(units, p.tile_wgs, kTileLeast);
+      const int per = (sh.G + 7) / 8;
+      me = die * per + in_die;
+      if (in_die >= per || me >= sh.G) return;
+      left = sh.first(me + 1) - sh.first(me);
+      if (me > 0) b = paged_locate(p.B, sh.first(me), all, reinterpret_cast<int*>(smem_raw), index, units);
+      b = __builtin_amdgcn_readfirstlane(b);
+      index = __builtin_amdgcn_readfirstlane(index);
+      units_b = tile_units(p, b);
+      rb = index / units_b;
+      unit = index % units_b;
+    }
+  }
+
+  for (int segment = 0; left > 0; ++segment) {
+  int row0 = 0, first = 0, nq, len = p.prefix, pages;             // first row of the sequence in [T * nH], its first key, ..
+  const int* table = p.prefix_table;
+  if constexpr (PREFIX) {
+    nq = min(max(p.q_start[p.B], 0), p.T);
+    pages = divide(p.prefix - 1, p.ps) + 1;
+    if (rb * RB >= nq * p.nH) return;
+  } else {
     const PagedSeq s = paged_seq(p, b);
     nq = s.nq;
     row0 = s.q0 * p.nH;
-    n_rows = nq * p.nH;
     first = p.prefix;
     len = s.len;
     table = p.table + (long)b * p.max_pages;
     pages = p.max_pages;
   }
+  const int n_rows = nq * p.nH, now = PREFIX ? 1 : min(left, units_b - unit);
   const bool causal = !PREFIX && p.causal;
   const int r0 = rb * RB, rw = r0 + wave * 32;                 // first row of the workgroup, of this wave
   const int r = min(rw + lr, n_rows - 1);                         // rows behind the last repeat it and are not stored
   auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
   const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);     // keys that the row sees, that all and any rows of the workgroup see
   const int hi = sees(rw + 31);                                   // keys that any row of the wave sees
-  const int tiles = hi_all > first ? (hi_all - first + BC - 1) / BC : 0;
-  const int per = (tiles + parts - 1) / parts;
-  const int k0 = part * per, cnt = max(min(tiles, k0 + per) - k0, 0);
-  const int key0 = first + k0 * BC;
+  const int key0 = PREFIX ? part * p.prefix_keys : first + unit * kTileUnit;
+  const int key1 = min(hi_all, PREFIX ? key0 + p.prefix_keys : key0 + now * kTileUnit);
+  const int cnt = key1 > key0 ? (key1 - key0 + BC - 1) / BC : 0;  // tiles
 
   f32x16 oacc[CB];
   float m_run = -INFINITY, l_run = 0.f;
@@ -94,13 +118,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
     constexpr float kLazy = 8.f;
     const int xs = swz_x<CPR>(lr);
-    // the 32 keys from key n0 on, rows kr .. of stage st; between(): work that is done while the first products run; careful: some
-    // rows may not see some of the keys
-    auto block = [&](auto careful, int n0, int kr, int st, auto between) {
-      constexpr bool CAREFUL = decltype(careful)::value;
+    // ---- a block of 32 keys, rows kr .. of stage st: scores, probabilities, O += V P ----
+    auto scores = [&](int kr, int st, f32x16& s) {
       const T* kt = smem + (long)st * L::kStage + kr * D;
-      const T* vt = kt + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
-      f32x16 s;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.f;
       constexpr int G = KIND == 1 && CB > 2 ? 2 : CB;             // channel blocks whose reads are all on their way before a product
@@ -120,14 +140,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      between();
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (CAREFUL) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit ? s[e] : -INFINITY;
-      }
-      // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the reference by
-      // more than kLazy (probabilities stay below 2^kLazy)
+    };
+    // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the reference by more
+    // than kLazy (probabilities stay below 2^kLazy)
+    auto probabilities = [&](f32x16& s) {
       float mx = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
@@ -146,38 +162,57 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e] * p.scale - m_use);
       l_run = block_sum(s, l_run);
-      const Frag<T> pf = to_frag<T>(s);
-      constexpr int TF = CB < 2 ? 1 : 2;
+      return to_frag<T>(s);
+    };
+    // some rows may not see some of the keys, n0 ..
+    auto values = [&](int n0, int kr, int st, const Frag<T>& pf) {
+      const T* vt = smem + (long)st * L::kStage + kr * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
 #pragma unroll
-      for (int k = 0; k < CB / TF; ++k) {
-        Frag<T> vf[TF];
-        load_frags_tr_swz<CPR>(vf, vt, 0, k * TF * 32, lane);
-        if constexpr (CAREFUL) {
-          bool fine = true;
-#pragma unroll
-          for (int f = 0; f < TF; ++f) fine = fine && frag_finite(vf[f]);
-          if (__builtin_amdgcn_ballot_w64(!fine) != 0ull) {       // (rare)
-#pragma unroll
-            for (int f = 0; f < TF; ++f) take_nonfinite<T>(vf[f], frag_seen(limit - n0 - 4 * h, T()), oacc[k * TF + f]);
-          }
-        }
-#pragma unroll
-        for (int f = 0; f < TF; ++f) mma32(oacc[k * TF + f], vf[f], pf);
+      for (int cb = 0; cb < CB; ++cb) {
+        Frag<T> vf[1];
+        load_frags_tr_swz<CPR>(vf, vt, 0, cb * 32, lane);
+        if (__builtin_amdgcn_ballot_w64(!frag_finite(vf[0])) != 0ull) take_nonfinite<T>(vf[0], limit - n0 - 4 * h, oacc[cb]);   // (rare)
+        mma32(oacc[cb], vf[0], pf);
       }
     };
-    // tile j from stage st: one that all rows of the workgroup see, and any other (a block that no row of the wave sees is passed over)
-    auto whole = [&](int j, int st, auto between) {
-      const int n0 = tile_at(j);
-      block(std::false_type(), n0, 0, st, between);
+    // A tile that all rows of the workgroup see: the products of one block run under the exponentials of the other.  between(): work
+    // that is done under the first products.
+    auto whole = [&](int st, auto between) {
+      f32x16 s[NB];
 #pragma unroll
-      for (int nb = 1; nb < NB; ++nb) block(std::false_type(), n0 + nb * 32, nb * 32, st, [] {});
-    };
-    auto edge = [&](int j, int st, auto between) {
-      const int n0 = tile_at(j);
+      for (int nb = 0; nb < NB; ++nb) scores(nb * 32, st, s[nb]);
       between();
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        __builtin_amdgcn_sched_barrier(0);
+        // the first value fragments are on their way under the exponentials
+        constexpr int TF = CB < 2 ? 1 : 2;
+        const T* vt = smem + (long)st * L::kStage + nb * 32 * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
+        Frag<T> vf[TF];
+        load_frags_tr_swz<CPR>(vf, vt, 0, 0, lane);
+        const Frag<T> pf = probabilities(s[nb]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < CB / TF; ++k) {
+          if (k > 0) load_frags_tr_swz<CPR>(vf, vt, 0, k * TF * 32, lane);
+#pragma unroll
+          for (int f = 0; f < TF; ++f) mma32(oacc[k * TF + f], vf[f], pf);
+        }
+      }
+    };
+    // any other, a block that no row of the wave sees passed over
+    auto edge = [&](int j, int st) {
 #pragma unroll 1
-      for (int nb = 0; nb < NB; ++nb)
-        if (n0 + nb * 32 < hi) block(std::true_type(), n0 + nb * 32, nb * 32, st, [] {});
+      for (int nb = 0; nb < NB; ++nb) {
+        const int n0 = tile_at(j) + nb * 32;
+        if (n0 >= hi) break;
+        f32x16 s;
+        scores(nb * 32, st, s);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit ? s[e] : -INFINITY;
+        const Frag<T> pf = probabilities(s);
+        values(n0, nb * 32, st, pf);
+      }
     };
     const int n_whole = min(max(lo_all - key0, 0) / BC, cnt);
 
@@ -189,64 +224,83 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const int n = min(tile_at(j) + lane, hi_all - 1);
         word_to_lds(table + min(divide(n, p.ps), pages - 1), entries + (j & 3) * 64);
       };
-      // A wave's pieces of a tile: 1 KB each, NK of the keys and as many, of the same rows, of the values.  Where this lane's
-      // chunks of them come from, in 16-byte units behind the pools' starts (a chunk behind the row's end: negative):
-      constexpr int NK = BC * D / 512 / 4;
-      const uint32_t k16 = (uint32_t)(p.k_stride / 8), v16 = (uint32_t)(p.v_stride / 8);
-      long kfrom[NK], vfrom[KIND == 0 ? NK : 1];
+      // A wave takes BC / 4 consecutive rows of a tile: NK pieces of 1 KB of the keys, and as many of the values.  Where they come
+      // from, in 16-byte units behind the pools' starts (32 bits: 64 GiB).
+      constexpr int NK = BC * D / 512 / 4, ROWS = BC / 4;
+      static_assert(ROWS == 16, "rows of a wave");
+      const uint32_t k16 = (uint32_t)(p.k_stride / 8), v16 = (uint32_t)(p.v_stride / 8), rk = p.r3 / 8, rv = p.rt3 / 8;
+      auto row_of = [](int l, int i) { return i * RPP + l / CPR; };                                 // of the wave's
+      auto chunk_of = [](int l, int i) { return (l % CPR) ^ swz_x<CPR>(i * RPP + l / CPR); };
+      // Rows that lie in one page and fill the tile's width: one start for the wave, and what its lanes add to it.  Rows behind the
+      // last are whatever the page holds.
+      const bool straight = p.page_size % ROWS == 0 && first % ROWS == 0 && p.r3 == D && (KIND != 0 || p.rt3 == D);
+      // (in bytes, of its first piece; the others' differ in two bits of the chunk and in the row)
+      const uint32_t add0 = row_of(lane, 0) * (D * 2) + chunk_of(lane, 0) * 16;
+      static_assert(swz_x<CPR>(RPP) == (NK > 1 ? 4 : swz_x<CPR>(RPP)), "four chunks a piece");
+      uint32_t kstart = 0, vstart = 0;
       auto find = [&](int j) {
-        const int* ids = entries + (j & 3) * 64;
-        int l = lane;
-        asm volatile("" : "+v"(l));                               // (rows and chunks of the pieces are formed afresh, not kept across the loop)
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-          const int row = (wave + 4 * i) * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(row);
-          const int n = min(tile_at(j) + row, hi_all - 1);
-          const uint32_t page = paged_page(ids[row], p.n_pages), at = n - divide(n, p.ps) * p.page_size;
-          kfrom[i] = (long)((unsigned long)page * k16 + (at * (uint32_t)(p.r3 / 8) + c));
-          if (c * 8 >= p.r3) kfrom[i] = -1;
-          if constexpr (KIND == 0) {
-            vfrom[i] = (long)((unsigned long)page * v16 + (at * (uint32_t)(p.rt3 / 8) + c));
-            if (c * 8 >= p.rt3) vfrom[i] = -1;
-          }
-        }
+        const int n = tile_at(j) + wave * ROWS;
+        const uint32_t page = paged_page(__builtin_amdgcn_readfirstlane(entries[(j & 3) * 64 + wave * ROWS]), p.n_pages);
+        const uint32_t at = n - divide(n, p.ps) * p.page_size;
+        kstart = page * k16 + at * rk;
+        if constexpr (KIND == 0) vstart = page * v16 + at * rv;
       };
       auto issue = [&](int st) {
-        T* kt = smem + (long)st * L::kStage;
-        auto source = [&](const void* pool, long at) {
-          const u32x4* from = static_cast<const u32x4*>(pool) + at;
-          return p.r3 == D && p.rt3 == D ? from : at < 0 ? paged_zeros : from;
-        };
+        T* kt = smem + (long)st * L::kStage + wave * NK * 512;
+        const char *k = static_cast<const char*>(p.K) + (unsigned long)kstart * 16, *v = static_cast<const char*>(p.V) + (unsigned long)vstart * 16;
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-          chunk_to_lds(source(p.K, kfrom[i]), kt + (wave + 4 * i) * 512);
-          if constexpr (KIND == 0) chunk_to_lds(source(p.V, vfrom[i]), kt + L::kTile + (wave + 4 * i) * 512);
+          const uint32_t add = (add0 ^ (64 * i)) + i * 1024;
+          chunk_to_lds(k + add, kt + i * 512);
+          if constexpr (KIND == 0) chunk_to_lds(v + add, kt + L::kTile + i * 512);
+        }
+      };
+      // Else every lane looks up its own row (those behind the last repeat it; chunks behind a row's end are zeros)
+      auto find_and_issue = [&](int j, int st) {
+        const int* ids = entries + (j & 3) * 64 + wave * ROWS;
+        T* kt = smem + (long)st * L::kStage + wave * NK * 512;
+#pragma unroll 1
+        for (int i = 0; i < NK; ++i) {
+          const uint32_t c = chunk_of(lane, i);
+          const int n = min(tile_at(j) + wave * ROWS + row_of(lane, i), hi_all - 1);
+          const uint32_t page = paged_page(ids[row_of(lane, i)], p.n_pages), at = n - divide(n, p.ps) * p.page_size;
+          const u32x4* k = static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + c);
+          chunk_to_lds(c < rk ? k : paged_zeros, kt + i * 512);
+          if constexpr (KIND == 0) {
+            const u32x4* v = static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + c);
+            chunk_to_lds(c < rv ? v : paged_zeros, kt + L::kTile + i * 512);
+          }
         }
       };
       fetch_entries(0);
       fetch_entries(1);
       fetch_entries(2);
       wait_vm<0>();                                               // entries, and plain loads out of the way of the counted ones
-      find(0);
-      issue(0);
-      fetch_entries(3);
-      find(1);
-      auto next = [&](int j) {
+      auto fill = [&](int j, int st) {
+        if (straight) issue(st);
+        else find_and_issue(j, st);
+        fetch_entries(j + 3);
+      };
+      if (straight) find(0);
+      fill(0, 0);
+      if (straight) find(1);
+      auto arrived = [] {
         wait_vm<1>();                                             // this wave's part of tile j is there (entries may be on their way),
         wait_lds();                                               // its reads of tile j - 1 are done
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        issue((j + 1) & 1);                                       // the stage of tile j - 1
-        fetch_entries(j + 4);
       };
       int j = 0;
       for (; j < n_whole; ++j) {
-        next(j);
-        whole(j, j & 1, [&] { find(j + 2); });
+        arrived();
+        fill(j + 1, (j + 1) & 1);                                 // into the stage of tile j - 1
+        whole(j & 1, [&] { if (straight) find(j + 2); });
       }
       for (; j < cnt; ++j) {
-        next(j);
-        edge(j, j & 1, [&] { find(j + 2); });
+        arrived();
+        if (straight) find(j + 1);
+        fill(j + 1, (j + 1) & 1);
+        edge(j, j & 1);
       }
       wait_vm<0>();                                               // tiles requested past the end still land in LDS
     } else {
@@ -300,31 +354,114 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         __syncthreads();
         store((j + 1) & 1);                                       // the stage of tile j - 1
         load(j + 2);
-        whole(j, j & 1, [] {});
+        whole(j & 1, [] {});
       }
       for (; j < cnt; ++j) {                                      // (nothing is kept in registers for later: they are all in use)
         __syncthreads();
         load(j + 1);
         store((j + 1) & 1);
-        edge(j, j & 1, [] {});
+        edge(j, j & 1);
       }
     }
   }
 
+  // ---- the rows: a result, or a part of one ----
   const float l = halves_sum(l_run);
-  if (rw + lr >= n_rows) return;
-  const long at = (long)row0 + rw + lr;
-  const bool direct = !PREFIX && p.own_parts == 0;
-  const long slot = (long)((PREFIX ? 0 : p.prefix_parts) + part) * p.T * p.nH + at;
+  const bool complete = !PREFIX && now == units_b;                // nobody else has keys of these rows
+  if (rw + lr < n_rows) {
+    const long at = (long)row0 + rw + lr;
+    const bool direct = complete && p.prefix_parts == 0;
+    const bool by_row = PREFIX || complete;
+    const long slot = by_row ? (long)(PREFIX ? part : p.prefix_parts) * p.T * p.nH + at : (2l * me + (segment > 0)) * RB + wave * 32 + lr;
+    float* po = by_row ? p.part_o : p.stream_o;
+    float2* pml = by_row ? p.part_ml : p.stream_ml;
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
+    for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 o = {oacc[cb][4 * q], oacc[cb][4 * q + 1], oacc[cb][4 * q + 2], oacc[cb][4 * q + 3]};
-      const int c = cb * 32 + 8 * q + 4 * h;
-      if (direct) paged_result<T>(p, at, c, m_run, l, o);
-      else paged_partial<D>(p.part_o, p.part_ml, slot, c, m_run, l, o);
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 o = {oacc[cb][4 * q], oacc[cb][4 * q + 1], oacc[cb][4 * q + 2], oacc[cb][4 * q + 3]};
+        const int c = cb * 32 + 8 * q + 4 * h;
+        if (direct) paged_result<T>(p, at, c, m_run, l, o);
+        else paged_partial<D>(po, pml, slot, c, m_run, l, o);
+      }
+  }
+  left -= now;
+  if (PREFIX || left == 0) break;
+  unit = 0;
+  if (++rb == tile_blocks(p, b)) {
+    rb = 0;
+    do ++b;
+    while (tile_blocks(p, b) == 0);                               // (units are left, so a sequence with some follows)
+    units_b = tile_units(p, b);
+  }
+  __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// The partial results of a row block: those of the prefix, and its own.  Grid: row blocks x groups of rows; a row by D/4 threads, or
+// by `groups` times as many.
+// ------------------------------------------------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int groups) {
+  using T = bf16;
+  constexpr int L = D / 4, SLOTS = 256 / L;
+  __shared__ int sh[8];
+  __shared__ float4 po[256];
+  __shared__ float2 pml[SLOTS];
+  const int tid = threadIdx.x, per = SLOTS / groups;
+  int rb, blocks, at_unit = 0, units = 1;
+  const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, i); }, sh, rb, blocks);
+  if (b < 0) return;
+  const PagedSeq s = paged_seq(p, b);
+  const int n_rows = min(s.nq * p.nH - rb * kTileRows, kTileRows);
+  if ((int)blockIdx.y * per >= n_rows) return;
+  int g0 = 0, g1 = 0;                                             // workgroups that share the block,
+  bool cut = false;                                               // the first of them behind another block
+  if (p.tile_wgs > 0) {
+    int before = 0, all = 0;
+    for (int i = tid; i < p.B; i += 256) {
+      const int n = tile_blocks(p, i) * tile_units(p, i);
+      all += n;
+      if (i < b) before += n;
     }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      all += __shfl_xor(all, d);
+      before += __shfl_xor(before, d);
+    }
+    if (tid % kWave == 0) {
+      sh[tid / kWave] = all;
+      sh[4 + tid / kWave] = before;
+    }
+    __syncthreads();
+    units = sh[0] + sh[1] + sh[2] + sh[3];
+    const int units_b = tile_units(p, b);
+    at_unit = sh[4] + sh[5] + sh[6] + sh[7] + rb * units_b;
+    const Shares share(units, p.tile_wgs, kTileLeast);
+    g0 = share.group(at_unit);
+    g1 = share.group(at_unit + units_b - 1);
+    cut = share.first(g0) < at_unit;
+  }
+  const bool complete = g0 == g1;                                 // one workgroup did it all
+  if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
+  const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
+  const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + rb * kTileRows + r;
+  RowSum sum;
+  if (r < n_rows) {
+    sum.add_parts(p.prefix_parts + (complete ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
+      ml = p.part_ml + i * rows + row;
+      o = p.part_o + (i * rows + row) * D + c;
+    });
+    if (!complete)
+      sum.add_parts(g1 - g0 + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
+        const long at = (2l * (g0 + i) + (cut && i == 0)) * kTileRows + r;
+        ml = p.stream_ml + at;
+        o = p.stream_o + at * D + c;
+      });
+  }
+  sum.add_groups(po, pml, slot, group, groups, per, L);
+  if (group == 0 && r < n_rows) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
 }
 
 template <int D, int KIND, bool PREFIX> static hipError_t tile_one(const PagedArgs& a, hipStream_t s) {
@@ -332,8 +469,9 @@ template <int D, int KIND, bool PREFIX> static hipError_t tile_one(const PagedAr
   auto kern = paged_tile_kernel<D, KIND, PREFIX>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
-  const int blocks = PREFIX ? (int)(((long)a.T * a.nH + kTileRows - 1) / kTileRows) : paged_rows_blocks(a, kTileRows);
-  hipLaunchKernelGGL(kern, dim3(blocks, PREFIX ? a.prefix_parts : a.own_parts > 0 ? a.own_parts : 1), dim3(256), smem, s, a);
+  const long blocks = PREFIX ? ((long)a.T * a.nH + kTileRows - 1) / kTileRows * a.prefix_parts : a.tile_wgs;
+  const uint32_t grid = !PREFIX && a.tile_wgs == 0 ? paged_rows_blocks(a, kTileRows) : (uint32_t)((blocks + 7) / 8 * 8);
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), smem, s, a);
   return hipGetLastError();
 }
 template <int D> static hipError_t tile_variant(const PagedArgs& a, bool prefix, hipStream_t s) {
@@ -346,6 +484,24 @@ hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s
     case 32: return tile_variant<32>(a, prefix_pass, s);
     case 64: return tile_variant<64>(a, prefix_pass, s);
     case 128: return tile_variant<128>(a, prefix_pass, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int D> static hipError_t tile_join_one(const PagedArgs& a, hipStream_t s) {
+  constexpr int SLOTS = 256 / (D / 4);
+  const int blocks = paged_rows_blocks(a, kTileRows), parts = a.prefix_parts + (a.tile_wgs > 0 ? a.tile_wgs / blocks : 0) + 1;
+  int groups = 1;                                                 // one for every 8 parts that a block has on average
+  while (groups < 8 && 8 * groups < parts) groups *= 2;
+  const int per = SLOTS / groups, most = kTileRows < a.max_new * a.nH ? kTileRows : a.max_new * a.nH;
+  hipLaunchKernelGGL(paged_tile_join_kernel<D>, dim3(blocks, (most + per - 1) / per), dim3(256), 0, s, a, groups);
+  return hipGetLastError();
+}
+hipError_t launch_paged_tile_join(const PagedArgs& a, hipStream_t s) {
+  switch (a.D) {
+    case 32: return tile_join_one<32>(a, s);
+    case 64: return tile_join_one<64>(a, s);
+    case 128: return tile_join_one<128>(a, s);
   }
   return hipErrorInvalidValue;
 }
