@@ -45,14 +45,17 @@ struct PagedArgs {
   int prefix_parts;             // parts 0 .. prefix_parts-1: the prefix
   int own_parts;                // then those of the sequence's own rows; 0: written to O directly
   int prefix_keys, own_keys;    // keys of such parts (a short sequence leaves the last parts empty: no output, a sum of 0)
-  // The keys of all sequences dealt to workgroups in equal shares (0: a workgroup for every sequence, or row block): of paged_stream,
-  // which takes a sequence's `hb` blocks of 32 rows at once, and of paged_tile.  Rows that several workgroups share leave partial
-  // results, [2 * workgroups][hb * 32 or kTileRows] rows.
-  int hb, stream_wgs, tile_wgs;
+  // The keys of all sequences dealt to this many workgroups (0: a workgroup for every sequence, or row block): of paged_stream, which
+  // takes a sequence's `hb` blocks of 32 rows at once and gives no workgroup less than stream_least units, and of paged_tile.
+  // Rows that several workgroups share leave partial results: [workgroups][hb * 32] rows, [2 * workgroups][kTileRows].
+  int hb, stream_wgs, stream_least, tile_wgs;
   float* stream_o;
   float2* stream_ml;
 };
-constexpr int kStreamUnit = 128, kStreamLeast = 2;   // keys of a unit of that kernel's work, least units of a workgroup
+constexpr int kStreamUnit = 128;       // keys of a unit of that kernel's work
+// workgroups that share B sequences where `wgs` are wanted: with few sequences no more than that, else every sequence's last part
+// may be one more
+inline int stream_grid(int B, int wgs) { return 2l * B <= wgs ? wgs : wgs + B; }
 
 // Latent rows into their pages, keys (and the per-head queries, if given) rotated to the tokens' positions
 struct PagedAppendArgs {

@@ -74,8 +74,12 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   a.own_parts = prefix > 0 ? 1 : 0;                               // rows that one workgroup does alone
   long shared = 0;                                                // rows of partial results that workgroups share
   if (a.hb > 0) {
-    if (keys > kStreamWhole) a.stream_wgs = c->n_cus;
-    shared = 2l * a.stream_wgs * a.hb * 32;
+    // (with a prefix a second launch joins the results anyway)
+    a.stream_least = prefix > 0 ? 1 : 2;
+    if (keys > (prefix > 0 ? kStreamUnit : kStreamWhole)) {
+      a.stream_wgs = c->n_cus;
+      shared = (long)stream_grid(b->B, a.stream_wgs) * a.hb * 32;
+    }
   } else if (tile) {
     const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
     if (units > kTileLeast && blocks * units < (1l << 31)) a.tile_wgs = 2 * c->n_cus;

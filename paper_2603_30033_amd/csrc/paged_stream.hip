@@ -3,9 +3,9 @@
 //
 // The cached rows are read once, in order, and every one serves all heads: 2 nH flops a byte, so HBM bounds it.  What counts is
 // that all compute units stream all the time:
-//   - The key rows of all sequences are cut into units of 128, one behind the other, and every workgroup takes an equal share of
-//     consecutive units, whatever sequences they belong to (it finds its first one by a scan over the lengths).  A share ends
-//     inside a sequence as often as not: such a part leaves (max, sum, output) of its rows, which paged_join adds up.
+//   - The key rows of a sequence are cut into units of 128 and dealt to workgroups, the same number to each whatever the
+//     sequence: as many as give every compute unit one workgroup.  (A workgroup finds its part by a scan over the lengths, which
+//     live on the device.)  Where several share a sequence each leaves (max, sum, output) of its rows, which paged_join adds up.
 //   - Wave w takes keys 32w .. 32w+31 of a unit and does all the work for them (scores of every row, its own running softmax,
 //     product with the values): nothing is shared between the waves while they stream, so there is no barrier in the loop.
 //   - Rows go from the pages straight into the wave's two LDS stages, two units ahead; the page numbers one unit before that.
@@ -31,6 +31,42 @@ __device__ __forceinline__ int stream_units(const PagedArgs& p, int b) {
   const PagedSeq s = paged_seq(p, b);
   return (int)(s.nq != 0) * max(1, (s.len - p.prefix + kUnit - 1) / kUnit);   // (no branch: the loads go together)
 }
+// sum of every thread's number; all 256 threads call, sh holds 4 words
+__device__ __forceinline__ int block_total(int x, int* sh) {
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) x += __shfl_xor(x, d);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = x;
+  __syncthreads();
+  return sh[0] + sh[1] + sh[2] + sh[3];
+}
+// Units of a workgroup.  One round of workgroups over the compute units if that can be had: the units' share of each, or, where the
+// sequences' last parts make too many of these, a share that is larger by as much.
+struct StreamShare {
+  const PagedArgs& p;
+  int mine;                                                       // units of sequence threadIdx.x
+  int units;                                                      // of a workgroup
+  __device__ __forceinline__ StreamShare(const PagedArgs& a, int* sh) : p(a) {
+    mine = (int)threadIdx.x < p.B ? stream_units(p, threadIdx.x) : 0;
+    auto total = [&](auto f) {
+      int n = (int)threadIdx.x < p.B ? f(mine) : 0;
+      for (int i = threadIdx.x + 256; i < p.B; i += 256) n += f(stream_units(p, i));
+      return block_total(n, sh);
+    };
+    const int all = total([](int n) { return n; });
+    units = max(p.stream_least, (all + p.stream_wgs - 1) / p.stream_wgs);
+    if (2 * p.B <= p.stream_wgs) {
+      const int t = units;
+      if (total([=](int n) { return (n + t - 1) / t; }) > p.stream_wgs)
+        units = max(units, (all + p.stream_wgs - p.B - 1) / (p.stream_wgs - p.B));
+    }
+  }
+  __device__ __forceinline__ int parts(int b) const {             // workgroups of sequence b
+    const int n = b == (int)threadIdx.x ? mine : stream_units(p, b);
+    return (n + units - 1) / units;
+  }
+};
+
 template <int D, int HB, int KIND>
 // (wide latents: LDS leaves one wave to a SIMD, which may then use all registers)
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, HB == 1 && D < 128 ? 2 : 1)))
@@ -44,31 +80,29 @@ void paged_stream_kernel(PagedArgs p) {
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, lr = lane % 32;
 
-  int b, off, left;                                               // sequence, unit in it, units still to do
+  int b, off = 0, cnt;                                            // sequence, first unit in it, units
   if (p.stream_wgs == 0) {                                        // a workgroup for every sequence
     b = blockIdx.x;
-    off = 0;
-    left = stream_units(p, b);
+    cnt = stream_units(p, b);
   } else {
-    int units;
-    b = paged_locate(p.B, 0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
+    int* sh = reinterpret_cast<int*>(smem_raw);
+    const StreamShare share(p, sh);
+    int part, all;
+    __syncthreads();
+    b = paged_locate(p.B, blockIdx.x, [&](int i) { return share.parts(i); }, sh, part, all);
     if (b < 0) return;
-    const Shares sh(units, p.stream_wgs, kStreamLeast);
-    if ((int)blockIdx.x >= sh.G) return;
-    const int u0 = sh.first(blockIdx.x);
-    left = sh.first(blockIdx.x + 1) - u0;
-    if (u0 > 0) b = paged_locate(p.B, u0, [&](int i) { return stream_units(p, i); }, reinterpret_cast<int*>(smem_raw), off, units);
+    b = __builtin_amdgcn_readfirstlane(b);
+    off = __builtin_amdgcn_readfirstlane(part) * share.units;
+    cnt = min(share.units, stream_units(p, b) - off);
   }
-  if (left == 0) return;
-  b = __builtin_amdgcn_readfirstlane(b);
-  off = __builtin_amdgcn_readfirstlane(off);
+  if (cnt == 0) return;
 
   T* wbase = reinterpret_cast<T*>(smem_raw) + (long)wave * 2 * L::kStage;
   f32x4* rowtab = reinterpret_cast<f32x4*>(smem_raw + L::kStages);
   int* entries = reinterpret_cast<int*>(smem_raw + L::kStages + L::kRows) + wave * 4 * 64;
-  for (int segment = 0; left > 0; ++segment) {
+  {
     const PagedSeq s = paged_seq(p, b);
-    const int all = stream_units(p, b), cnt = min(left, all - off);
+    const int all = stream_units(p, b);
     const int keys = s.len, n_rows = s.nq * p.nH, row0 = s.q0 * p.nH;
     const int unit0 = p.prefix + off * kUnit;                     // first key
     const int* table = p.table + (long)b * p.max_pages;
@@ -283,20 +317,13 @@ void paged_stream_kernel(PagedArgs p) {
     __syncthreads();
 
     const bool complete = off == 0 && cnt == all, direct = complete && p.prefix_parts == 0;
-    const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (2l * blockIdx.x + (segment > 0)) * (HB * 32);
+    const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (long)blockIdx.x * (HB * 32);
     float* po = complete ? p.part_o : p.stream_o;
     float2* pml = complete ? p.part_ml : p.stream_ml;
     join_waves<D, HB>(reinterpret_cast<float*>(smem_raw), oacc, m_run, l_run, n_rows, [&](int row, int c, float m, float l, f32x4 o) {
       if (direct) paged_result<T>(p, (long)row0 + row, c, m, l, o);
       else paged_partial<D>(po, pml, slot0 + row, c, m, l, o);
     });
-    left -= cnt;
-    if (left > 0) {
-      off = 0;
-      do ++b;
-      while (stream_units(p, b) == 0);                            // (units are left, so a sequence with some follows)
-      __syncthreads();
-    }
   }
 }
 
@@ -316,32 +343,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups
   const int n_rows = s.nq * p.nH, per = SLOTS / groups;
   if ((int)blockIdx.y * per >= n_rows) return;
 
-  int g0 = 0, g1 = 0;                                             // workgroups that share the sequence,
-  bool cut = false;                                               // the first of them behind another sequence
+  int g0 = 0, own = 1;                                            // first of the workgroups that share the sequence, their number
   if (p.stream_wgs > 0) {
-    int before = 0, all = 0;
-    for (int i = tid; i < p.B; i += 256) {
-      const int n = stream_units(p, i);
-      all += n;
-      if (i < b) before += n;
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      all += __shfl_xor(all, d);
-      before += __shfl_xor(before, d);
-    }
-    if (tid % kWave == 0) {
-      sums[tid / kWave] = all;
-      sums[4 + tid / kWave] = before;
-    }
-    __syncthreads();
-    const int units = sums[0] + sums[1] + sums[2] + sums[3], u0 = sums[4] + sums[5] + sums[6] + sums[7];
-    const Shares sh(units, p.stream_wgs, kStreamLeast);
-    g0 = sh.group(u0);
-    g1 = sh.group(u0 + stream_units(p, b) - 1);
-    cut = sh.first(g0) < u0;
+    const StreamShare share(p, sums);
+    int before = 0;
+    for (int i = tid; i < b; i += 256) before += share.parts(i);
+    g0 = block_total(before, sums);
+    own = (stream_units(p, b) + share.units - 1) / share.units;
   }
-  const bool complete = g0 == g1;                                 // one workgroup did it all
+  const bool complete = own == 1;                                 // one workgroup did it all
   if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
   const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
   const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + r;
@@ -352,8 +362,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups
       o = p.part_o + (i * rows + row) * D + c;
     });
     if (!complete)
-      sum.add_parts(g1 - g0 + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
-        const long at = (2l * (g0 + i) + (cut && i == 0)) * (p.hb * 32) + r;
+      sum.add_parts(own, group, groups, [&](int i, const float2*& ml, const float*& o) {
+        const long at = (long)(g0 + i) * (p.hb * 32) + r;
         ml = p.stream_ml + at;
         o = p.stream_o + at * D + c;
       });
@@ -368,7 +378,7 @@ template <int D, int HB, int KIND> static hipError_t stream_one(const PagedArgs&
   auto kern = paged_stream_kernel<D, HB, KIND>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(a.stream_wgs > 0 ? a.stream_wgs : a.B), dim3(256), smem, s, a);
+  hipLaunchKernelGGL(kern, dim3(a.stream_wgs > 0 ? stream_grid(a.B, a.stream_wgs) : a.B), dim3(256), smem, s, a);
   return hipGetLastError();
 }
 template <int D> static hipError_t stream_variant(const PagedArgs& a, hipStream_t s) {
