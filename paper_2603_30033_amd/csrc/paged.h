@@ -53,6 +53,8 @@ struct PagedArgs {
   float2* stream_ml;
 };
 constexpr int kStreamUnit = 128;       // keys of a unit of that kernel's work
+// whether two of its workgroups share a compute unit by design (KIND 1: one pool, keys rotated on use)
+constexpr bool stream_late(int D, int kind) { return D == 128 && kind == 1; }
 // workgroups that share B sequences where `wgs` are wanted: with few sequences no more than that, else every sequence's last part
 // may be one more
 inline int stream_grid(int B, int wgs) { return 2l * B <= wgs ? wgs : wgs + B; }

@@ -77,7 +77,7 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     // (with a prefix a second launch joins the results anyway)
     a.stream_least = prefix > 0 ? 1 : 2;
     if (keys > (prefix > 0 ? kStreamUnit : kStreamWhole)) {
-      a.stream_wgs = c->n_cus;
+      a.stream_wgs = (stream_late(c->D, f.shared_kv && f.use_rope ? 1 : 0) ? 2 : 1) * c->n_cus;
       shared = (long)stream_grid(b->B, a.stream_wgs) * a.hb * 32;
     }
   } else if (tile) {

@@ -130,12 +130,7 @@ template <typename T> __device__ __forceinline__ Frag<T> rest_of(const f32x16& p
   return to_frag<T>(r);
 }
 
-// 16 bytes of zeros, which stand for the channels between a row's end and the tile's width
-static __device__ const u32x4 paged_zeros[1] = {{0u, 0u, 0u, 0u}};
-// lane l's 16 bytes (4 bytes) at `from` to chunk (word) l of `to` (the same for the whole wave)
-__device__ __forceinline__ void word_to_lds(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
-}
+// lane l's 16 bytes at `from` to chunk l of `to` (the same for the whole wave)
 __device__ __forceinline__ void chunk_to_lds(const void* from, void* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }

@@ -8,7 +8,7 @@
 //     live on the device.)  Where several share a sequence each leaves (max, sum, output) of its rows, which paged_join adds up.
 //   - Wave w takes keys 32w .. 32w+31 of a unit and does all the work for them (scores of every row, its own running softmax,
 //     product with the values): nothing is shared between the waves while they stream, so there is no barrier in the loop.
-//   - Rows go from the pages straight into the wave's two LDS stages, two units ahead; the page numbers one unit before that.
+//   - Rows go from the pages straight into the wave's two LDS stages, two units ahead.
 #include "paged_block.h"
 
 namespace ta {
@@ -20,9 +20,8 @@ template <int D, int KIND> struct StreamLds {
   static constexpr int kTile = 32 * D;                            // elements of 32 rows
   static constexpr int kStage = kTile * (KIND == 0 ? 2 : 1) + (KIND == 1 ? 512 : 0);   // KIND 1: 1 KB of rotation entries
   static constexpr size_t kStages = 4ul * 2 * kStage * sizeof(bf16);
-  static constexpr size_t kRows = KIND == 1 ? (size_t)(D / 4) * 32 * 16 : 0;           // rotation by 0 .. 31, behind the stages
-  static constexpr size_t kEntries = 4ul * 4 * 64 * sizeof(int);  // table entries of four blocks a wave, behind those
-  static constexpr size_t kAll = kStages + kRows + kEntries;
+  static constexpr size_t kRows = KIND == 1 ? (size_t)(D / 4) * 16 * 16 : 0;           // rotation by 0 .. 15, behind the stages
+  static constexpr size_t kAll = kStages + kRows;
   template <int HB> static constexpr size_t bytes() { return kAll > join_bytes<D, HB>() ? kAll : join_bytes<D, HB>(); }
 };
 
@@ -68,14 +67,15 @@ struct StreamShare {
 };
 
 template <int D, int HB, int KIND>
-// (wide latents: LDS leaves one wave to a SIMD, which may then use all registers)
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, HB == 1 && D < 128 ? 2 : 1)))
+// Wide latents with two pools: LDS leaves one wave to a SIMD, which may then use all registers.  With one pool whose keys are rotated on
+// use the vector unit is busier than memory: two workgroups share a compute unit, and a stage is filled again at a round's end.
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(stream_late(D, KIND) ? 2 : 1, HB == 1 && (D < 128 || KIND == 1) ? 2 : 1)))
 void paged_stream_kernel(PagedArgs p) {
   using T = bf16;
   using L = StreamLds<D, KIND>;
   constexpr int CB = D / 32, CPR = D / 8, RPP = 64 / CPR;         // 16-byte chunks of a row, rows of a 1 KB piece
   constexpr int PIECES = L::kTile / 512;
-  constexpr bool ROT = KIND == 1;
+  constexpr bool ROT = KIND == 1, kLate = stream_late(D, KIND);
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int h = lane / 32, lr = lane % 32;
@@ -99,232 +99,240 @@ void paged_stream_kernel(PagedArgs p) {
 
   T* wbase = reinterpret_cast<T*>(smem_raw) + (long)wave * 2 * L::kStage;
   f32x4* rowtab = reinterpret_cast<f32x4*>(smem_raw + L::kStages);
-  int* entries = reinterpret_cast<int*>(smem_raw + L::kStages + L::kRows) + wave * 4 * 64;
-  {
-    const PagedSeq s = paged_seq(p, b);
-    const int all = stream_units(p, b);
-    const int keys = s.len, n_rows = s.nq * p.nH, row0 = s.q0 * p.nH;
-    const int unit0 = p.prefix + off * kUnit;                     // first key
-    const int* table = p.table + (long)b * p.max_pages;
-    const int lo = p.causal ? keys - s.nq + 1 : keys;             // keys that every row sees
+  const PagedSeq s = paged_seq(p, b);
+  const int all = stream_units(p, b);
+  const int keys = s.len, n_rows = s.nq * p.nH, row0 = s.q0 * p.nH;
+  const int unit0 = p.prefix + off * kUnit;                     // first key
+  const int* table = p.table + (long)b * p.max_pages;
+  const int lo = p.causal ? keys - s.nq + 1 : keys;             // keys that every row sees
 
-    f32x16 oacc[HB][CB];
-    float m_run[HB], l_run[HB];
-    int limit[HB];                                                // keys that this lane's row sees
+  f32x16 oacc[HB][CB];
+  float m_run[HB], l_run[HB];
+  int limit[HB];                                                // keys that this lane's row sees
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) {
+    m_run[hb] = -INFINITY;
+    l_run[hb] = 0.f;
+    limit[hb] = p.causal ? lo + divide(min(hb * 32 + lr, n_rows - 1), p.heads) : keys;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) oacc[hb][cb][e] = 0.f;
+  }
+
+  if (unit0 < keys) {                                           // (the same for the whole workgroup)
+    // 16 rows in one page (the usual sizes): their number comes by a scalar read, there is one start for the wave, and lanes add
+    // their row and chunk to it.  Rows behind the sequence's last are whatever the page holds, chunks behind a row's end (which meet
+    // zeros of the queries, or become channels that are not stored) repeat its last.  Else every lane looks up its own rows.
+    constexpr int PPG = 16 / RPP;                                 // pieces of 16 rows
+    const bool straight = p.page_size % 16 == 0 && p.prefix % 16 == 0;
+    auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
+    const auto* entries = (const __attribute__((address_space(4))) int*)table;
+    auto entry_at = [&](int j, int half) {
+      return entries[min(divide(min(block_at(j) + 16 * half, keys - 1), p.ps), p.max_pages - 1)];
+    };
+    int entry[2] = {entry_at(0, 0), entry_at(0, 1)};              // of the block that is issued next
+    auto issue = [&](int j, int st) {
+      const int n0 = block_at(j);
+      T* kt = wbase + (long)st * L::kStage;
+      int l = lane;
+      asm volatile("" : "+v"(l));                                 // (chunks of the pieces are formed afresh, not kept across the loop)
+      if (straight) {
+        const char *k = nullptr, *v = nullptr;
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+          if (q % PPG == 0) {                                     // the next 16 rows
+            const int n = n0 + q * RPP;
+            const long pg = paged_page(entry[q / PPG], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
+            k = static_cast<const char*>(p.K) + (pg * p.k_stride + a * p.r3) * 2;
+            if constexpr (KIND == 0) v = static_cast<const char*>(p.V) + (pg * p.v_stride + a * p.rt3) * 2;
+          }
+          const uint32_t row = q % PPG * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(q * RPP + l / CPR);
+          chunk_to_lds(k + row * (p.r3 * 2) + min(c * 16, p.r3 * 2u - 16), kt + q * 512);
+          if constexpr (KIND == 0) chunk_to_lds(v + row * (p.rt3 * 2) + min(c * 16, p.rt3 * 2u - 16), kt + L::kTile + q * 512);
+        }
+        entry[0] = entry_at(j + 1, 0);
+        entry[1] = entry_at(j + 1, 1);
+      } else {
+#pragma unroll 1
+        for (int q = 0; q < PIECES; ++q) {
+          const int row = q * RPP + l / CPR, c = ((l % CPR) ^ swz_x<CPR>(row)) * 8;
+          const int n = min(n0 + row, keys - 1), i = divide(n, p.ps);
+          const long pg = paged_page(table[min(i, p.max_pages - 1)], p.n_pages), a = n - i * p.page_size;
+          const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3;
+          chunk_to_lds(kp + min(c, p.r3 - 8), kt + q * 512);
+          if constexpr (KIND == 0) {
+            const T* vp = static_cast<const T*>(p.V) + pg * p.v_stride + a * p.rt3;
+            chunk_to_lds(vp + min(c, p.rt3 - 8), kt + L::kTile + q * 512);
+          }
+        }
+      }
+      if constexpr (ROT) {                                        // rotation of the block's rows 0 and 16
+        const int quad = l % (D / 4), n = n0 + 16 * (l / (D / 4) % 2);
+        chunk_to_lds(reinterpret_cast<const f32x4*>(p.rope) + (long)quad * p.rope_ld + min(n, p.rope_ld - 1), kt + L::kTile);
+      }
+    };
+    // vector-memory operations behind those of block j when round j begins (looking up rows one by one: those at least)
+    constexpr int OPS = PIECES * (KIND == 0 ? 2 : 1) + (ROT ? 1 : 0);
+
+    Frag<T> qf[HB][CB];
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
-      m_run[hb] = -INFINITY;
-      l_run[hb] = 0.f;
-      limit[hb] = p.causal ? lo + divide(min(hb * 32 + lr, n_rows - 1), p.heads) : keys;
+      const T* q = static_cast<const T*>(p.Q) + (long)(row0 + min(hb * 32 + lr, n_rows - 1)) * p.q_row;
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[hb][cb][e] = 0.f;
+      for (int cb = 0; cb < CB; ++cb) qf[hb][cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
     }
+    if constexpr (ROT) {
+      for (int i = threadIdx.x; i < (D / 4) * 16; i += 256)
+        rowtab[i] = reinterpret_cast<const f32x4*>(p.rope)[(long)(i / 16) * p.rope_ld + min(i % 16, p.rope_ld - 1)];
+    }
+    wait_vm<0>();                                               // plain loads out of the way of the counted ones
+    wait_lds();
+    if constexpr (ROT) __syncthreads();
+    issue(0, 0);
+    issue(1, 1);
 
-    if (unit0 < keys) {                                           // (the same for the whole workgroup)
-      // 16 rows in one page that fill the tile's width: one start for the wave, and what its lanes add to it (in bytes, of the first
-      // piece; the others' differ in two bits of the chunk and in the row).  Rows behind the sequence's last are whatever the page
-      // holds.  Else every lane looks up its own row.
-      constexpr int PPG = 16 / RPP;
-      static_assert(PPG == 1 || swz_x<CPR>(RPP) == 4, "four chunks a piece");
-      const bool straight = p.page_size % 16 == 0 && p.prefix % 16 == 0 && p.r3 == D && (KIND != 0 || p.rt3 == D);
-      const uint32_t add0 = lane / CPR * (D * 2) + ((lane % CPR) ^ swz_x<CPR>(lane / CPR)) * 16;
-      auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
-      // The table entries of block j's rows come by way of LDS too: an entry in a register would be waited for with every tile
-      // behind it.  Rows behind the last repeat it and are masked.
-      auto fetch_entries = [&](int j) {
-        const int n = min(block_at(j) + lr, keys - 1);
-        word_to_lds(table + min(divide(n, p.ps), p.max_pages - 1), entries + (j & 3) * 64);
-      };
-      auto issue = [&](int j, int st) {
-        const int n0 = block_at(j);
-        const int* ids = entries + (j & 3) * 64;
-        T* kt = wbase + (long)st * L::kStage;
-        if (straight) {
-          const char *k = nullptr, *v = nullptr;
+    constexpr float kLazy = 8.f;
+    const int xs = swz_x<CPR>(lr);
+    auto round = [&](int j, int st) {
+      const int n0 = block_at(j);
+      const T* kt = wbase + (long)st * L::kStage;
+      wait_vm<OPS>();
+      f32x16 sc[HB];
 #pragma unroll
-          for (int q = 0; q < PIECES; ++q) {
-            if (q % PPG == 0) {                                   // the next 16 rows: they lie in one page
-              const int row = q * RPP, n = n0 + row;
-              const long pg = paged_page(__builtin_amdgcn_readfirstlane(ids[row]), p.n_pages), a = n - divide(n, p.ps) * p.page_size;
-              k = static_cast<const char*>(p.K) + (pg * p.k_stride + a * D) * 2;
-              if constexpr (KIND == 0) v = static_cast<const char*>(p.V) + (pg * p.v_stride + a * D) * 2;
-            }
-            const uint32_t add = (add0 ^ (64 * (q % PPG))) + q % PPG * 1024;
-            chunk_to_lds(k + add, kt + q * 512);
-            if constexpr (KIND == 0) chunk_to_lds(v + add, kt + L::kTile + q * 512);
-          }
-        } else {
-#pragma unroll 1
-          for (int q = 0; q < PIECES; ++q) {
-            const int row = q * RPP + lane / CPR, c = ((lane % CPR) ^ swz_x<CPR>(row)) * 8;
-            const int n = min(n0 + row, keys - 1);
-            const long pg = paged_page(ids[row], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
-            const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3 + c;
-            chunk_to_lds(c < p.r3 ? kp : reinterpret_cast<const T*>(paged_zeros), kt + q * 512);
-            if constexpr (KIND == 0) {
-              const T* vp = static_cast<const T*>(p.V) + pg * p.v_stride + a * p.rt3 + c;
-              chunk_to_lds(c < p.rt3 ? vp : reinterpret_cast<const T*>(paged_zeros), kt + L::kTile + q * 512);
-            }
-          }
-        }
-        if constexpr (ROT) {
-          const f32x4* tab = reinterpret_cast<const f32x4*>(p.rope) + (long)min(lr, D / 4 - 1) * p.rope_ld + min(n0, p.rope_ld - 1);
-          chunk_to_lds(tab, kt + L::kTile);
-        }
-      };
-      // vector-memory operations behind those of block j when round j begins: entries, a stage, entries
-      constexpr int OPS = PIECES * (KIND == 0 ? 2 : 1) + (ROT ? 1 : 0) + 2;
-
-      fetch_entries(0);
-      fetch_entries(1);
-      fetch_entries(2);
-      Frag<T> qf[HB][CB];
+      for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-      for (int hb = 0; hb < HB; ++hb) {
-        const T* q = static_cast<const T*>(p.Q) + (long)(row0 + min(hb * 32 + lr, n_rows - 1)) * p.q_row;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) qf[hb][cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
-      }
+        for (int e = 0; e < 16; ++e) sc[hb][e] = 0.f;
       if constexpr (ROT) {
-        for (int i = threadIdx.x; i < (D / 4) * 32; i += 256)
-          rowtab[i] = reinterpret_cast<const f32x4*>(p.rope)[(long)(i / 32) * p.rope_ld + min(i % 32, p.rope_ld - 1)];
-      }
-      wait_vm<0>();                                               // entries, and plain loads out of the way of the counted ones
-      wait_lds();
-      if constexpr (ROT) __syncthreads();
-      issue(0, 0);
-      fetch_entries(3);
-      issue(1, 1);
-
-      constexpr float kLazy = 8.f;
-      const int xs = swz_x<CPR>(lr);
-      auto round = [&](int j, int st) {
-        const int n0 = block_at(j);
-        const T* kt = wbase + (long)st * L::kStage;
-        wait_vm<OPS>();
-        f32x16 sc[HB];
+        const f32x4* rl = reinterpret_cast<const f32x4*>(kt + L::kTile);
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb)
+        for (int cb = 0; cb < CB; ++cb) {
+          const Frag<T> raw = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
+          f32x16 x;                                             // the row's 16 channels, turned by (key 0 or 16 of the block) + (row)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sc[hb][e] = 0.f;
-        if constexpr (ROT) {
-          const f32x4* rl = reinterpret_cast<const f32x4*>(kt + L::kTile);
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 t = rl[lr / 16 * (D / 4) + 8 * cb + 4 * h + q], a = rowtab[(8 * cb + 4 * h + q) * 16 + lr % 16];
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) {
-            const Frag<T> raw = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
-            f32x16 x;                                             // the row's 16 channels, turned by (first key of the block) + (row)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const f32x4 t = rl[8 * cb + 4 * h + q], a = rowtab[(8 * cb + 4 * h + q) * 32 + lr];
-#pragma unroll
-              for (int e = 0; e < 4; e += 2) {
-                const float c = a[e] * t[e] - a[e + 1] * t[e + 1], sn = a[e + 1] * t[e] + a[e] * t[e + 1];
-                const float x0 = frag_at(raw, 4 * q + e), x1 = frag_at(raw, 4 * q + e + 1);
-                x[4 * q + e] = x0 * c - x1 * sn;
-                x[4 * q + e + 1] = x0 * sn + x1 * c;
-              }
-            }
-            const Frag<T> kf = to_frag<T>(x), rest = rest_of<T>(x, kf);
-#pragma unroll
-            for (int hb = 0; hb < HB; ++hb) {
-              mma32(sc[hb], kf, qf[hb][cb]);
-              mma32(sc[hb], rest, qf[hb][cb]);
+            for (int e = 0; e < 4; e += 2) {
+              const float c = a[e] * t[e] - a[e + 1] * t[e + 1], sn = a[e + 1] * t[e] + a[e] * t[e + 1];
+              const float x0 = frag_at(raw, 4 * q + e), x1 = frag_at(raw, 4 * q + e + 1);
+              x[4 * q + e] = x0 * c - x1 * sn;
+              x[4 * q + e + 1] = x0 * sn + x1 * c;
             }
           }
-        } else {
+          const Frag<T> kf = to_frag<T>(x), rest = rest_of<T>(x, kf);
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) {
-            const Frag<T> kf = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
-#pragma unroll
-            for (int hb = 0; hb < HB; ++hb) mma32(sc[hb], kf, qf[hb][cb]);
+          for (int hb = 0; hb < HB; ++hb) {
+            mma32(sc[hb], kf, qf[hb][cb]);
+            mma32(sc[hb], rest, qf[hb][cb]);
           }
         }
-        // the value fragments (transposing reads) are taken before the stage is filled again
-        constexpr int TF = CB < 2 ? 1 : 2;
-        Frag<T> vf[CB / TF][TF];
+      } else {
 #pragma unroll
-        for (int k = 0; k < CB / TF; ++k) load_frags_tr_swz<CPR, false>(vf[k], kt + (KIND == 0 ? L::kTile : 0), 0, k * TF * 32, lane);
+        for (int cb = 0; cb < CB; ++cb) {
+          const Frag<T> kf = load_frag_swz<T>(kt + lr * D, 4 * cb + 2 * h, xs);
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) mma32(sc[hb], kf, qf[hb][cb]);
+        }
+      }
+      // the value fragments (transposing reads) are taken before the stage is filled again
+      constexpr int TF = CB < 2 ? 1 : 2;
+      Frag<T> vf[CB / TF][TF];
+      const T* vt = kt + (KIND == 0 ? L::kTile : 0);
+      if constexpr (!kLate) {
+#pragma unroll
+        for (int k = 0; k < CB / TF; ++k) load_frags_tr_swz<CPR, false>(vf[k], vt, 0, k * TF * 32, lane);
         wait_lds();
         issue(j + 2, st);
+      }
 
-        const bool partly = n0 + 32 > lo;
+      const bool partly = n0 + 32 > lo;
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
+      for (int hb = 0; hb < HB; ++hb) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sc[hb][e] *= p.scale;
-          if (partly)
+        for (int e = 0; e < 16; ++e) sc[hb][e] *= p.scale;
+        if (partly)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sc[hb][e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit[hb] ? sc[hb][e] : -INFINITY;
-        }
-        // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the
-        // reference by more than kLazy (probabilities stay below 2^kLazy)
-        Frag<T> pf[HB], ph[HB];
+          for (int e = 0; e < 16; ++e) sc[hb][e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit[hb] ? sc[hb][e] : -INFINITY;
+      }
+      // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the
+      // reference by more than kLazy (probabilities stay below 2^kLazy)
+      Frag<T> pf[HB], ph[HB];
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
-          float mx = -INFINITY;
+      for (int hb = 0; hb < HB; ++hb) {
+        float mx = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[hb][e]);
-          mx = halves_max(mx);
-          const bool raise = mx > m_run[hb] + kLazy;              // -inf + kLazy = -inf: the first block with a key raises
-          if (__builtin_amdgcn_ballot_w64(raise) != 0ull) {
-            const float alpha = raise ? fast_exp2(m_run[hb] - mx) : 1.f;
-            if (raise) m_run[hb] = mx;
-            l_run[hb] *= alpha;
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) oacc[hb][cb][e] *= alpha;
-          }
-          const float m_use = m_run[hb] == -INFINITY ? 0.f : m_run[hb];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sc[hb][e] = fast_exp2(sc[hb][e] - m_use);
-          l_run[hb] = block_sum(sc[hb], l_run[hb]);
-          pf[hb] = to_frag<T>(sc[hb]);
-          ph[hb] = rest_of<T>(sc[hb], pf[hb]);
-        }
-        bool fine = true;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) fine = fine && frag_finite(vf[cb / TF][cb % TF]);
-        if (__builtin_amdgcn_ballot_w64(!fine) == 0ull) {
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[hb][e]);
+        mx = halves_max(mx);
+        const bool raise = mx > m_run[hb] + kLazy;              // -inf + kLazy = -inf: the first block with a key raises
+        if (__builtin_amdgcn_ballot_w64(raise) != 0ull) {
+          const float alpha = raise ? fast_exp2(m_run[hb] - mx) : 1.f;
+          if (raise) m_run[hb] = mx;
+          l_run[hb] *= alpha;
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-            for (int hb = 0; hb < HB; ++hb) {
-              mma32(oacc[hb][cb], vf[cb / TF][cb % TF], pf[hb]);
-              mma32(oacc[hb][cb], vf[cb / TF][cb % TF], ph[hb]);
-            }
-        } else {
+            for (int e = 0; e < 16; ++e) oacc[hb][cb][e] *= alpha;
+        }
+        const float m_use = m_run[hb] == -INFINITY ? 0.f : m_run[hb];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[hb][e] = fast_exp2(sc[hb][e] - m_use);
+        l_run[hb] = block_sum(sc[hb], l_run[hb]);
+        pf[hb] = to_frag<T>(sc[hb]);
+        ph[hb] = rest_of<T>(sc[hb], pf[hb]);
+      }
+      if constexpr (kLate) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          Frag<T> v[1];
+          load_frags_tr_swz<CPR>(v, vt, 0, cb * 32, lane);
+          if (__builtin_amdgcn_ballot_w64(!frag_finite(v[0])) != 0ull) take_nonfinite<T>(v[0], limit[0] - n0 - 4 * h, oacc[0][cb]);
+          mma32(oacc[0][cb], v[0], pf[0]);
+          mma32(oacc[0][cb], v[0], ph[0]);
+        }
+        wait_lds();
+        issue(j + 2, st);
+        return;
+      }
+      bool fine = true;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) fine = fine && frag_finite(vf[cb / TF][cb % TF]);
+      if (__builtin_amdgcn_ballot_w64(!fine) == 0ull) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb) {
+            mma32(oacc[hb][cb], vf[cb / TF][cb % TF], pf[hb]);
+            mma32(oacc[hb][cb], vf[cb / TF][cb % TF], ph[hb]);
+          }
+      } else {
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-              Frag<T> v = vf[cb / TF][cb % TF];
-              take_nonfinite<T>(v, limit[hb] - n0 - 4 * h, oacc[hb][cb]);
-              mma32(oacc[hb][cb], v, pf[hb]);
-              mma32(oacc[hb][cb], v, ph[hb]);
-            }
+        for (int hb = 0; hb < HB; ++hb) {
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            Frag<T> v = vf[cb / TF][cb % TF];
+            take_nonfinite<T>(v, limit[hb] - n0 - 4 * h, oacc[hb][cb]);
+            mma32(oacc[hb][cb], v, pf[hb]);
+            mma32(oacc[hb][cb], v, ph[hb]);
           }
         }
-      };
-      for (int j = 0; j < cnt; ++j) {
-        fetch_entries(j + 4);
-        round(j, j & 1);
       }
-      wait_vm<0>();                                               // tiles requested past the end still land in LDS
+    };
+    for (int j = 0; j < cnt; ++j) {
+      round(j, j & 1);
     }
-    __syncthreads();
-
-    const bool complete = off == 0 && cnt == all, direct = complete && p.prefix_parts == 0;
-    const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (long)blockIdx.x * (HB * 32);
-    float* po = complete ? p.part_o : p.stream_o;
-    float2* pml = complete ? p.part_ml : p.stream_ml;
-    join_waves<D, HB>(reinterpret_cast<float*>(smem_raw), oacc, m_run, l_run, n_rows, [&](int row, int c, float m, float l, f32x4 o) {
-      if (direct) paged_result<T>(p, (long)row0 + row, c, m, l, o);
-      else paged_partial<D>(po, pml, slot0 + row, c, m, l, o);
-    });
+    wait_vm<0>();                                               // tiles requested past the end still land in LDS
   }
+  __syncthreads();
+
+  const bool complete = off == 0 && cnt == all, direct = complete && p.prefix_parts == 0;
+  const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (long)blockIdx.x * (HB * 32);
+  float* po = complete ? p.part_o : p.stream_o;
+  float2* pml = complete ? p.part_ml : p.stream_ml;
+  join_waves<D, HB>(reinterpret_cast<float*>(smem_raw), oacc, m_run, l_run, n_rows, [&](int row, int c, float m, float l, f32x4 o) {
+    if (direct) paged_result<T>(p, (long)row0 + row, c, m, l, o);
+    else paged_partial<D>(po, pml, slot0 + row, c, m, l, o);
+  });
 }
 
 // ------------------------------------------------------------------------------------------------------------------

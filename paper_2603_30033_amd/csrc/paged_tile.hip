@@ -17,9 +17,7 @@ template <int D, int KIND> struct TileLds {
   static constexpr int kKeys = KIND == 1 ? 32 : 64;               // of a tile
   static constexpr int kTile = kKeys * D;                         // elements
   static constexpr int kStage = kTile * (KIND == 0 ? 2 : KIND == 1 ? 3 : 1);
-  static constexpr size_t kEntries = KIND == 1 ? 0 : 4ul * 4 * 64 * sizeof(int);      // table entries of four tiles a wave
-  static constexpr size_t kTiles = 2ul * kStage * sizeof(bf16);
-  static constexpr size_t kBytes = kTiles + kEntries;
+  static constexpr size_t kBytes = 2ul * kStage * sizeof(bf16);
 };
 
 // row blocks of sequence b, and units of keys of each of them (no key of its own: one, which leaves the rows' empty result).  Rows that
@@ -175,13 +173,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         mma32(oacc[cb], vf[0], pf);
       }
     };
-    // A tile that all rows of the workgroup see: the products of one block run under the exponentials of the other.  between(): work
-    // that is done under the first products.
-    auto whole = [&](int st, auto between) {
+    // A tile that all rows of the workgroup see: the products of one block run under the exponentials of the other.
+    auto whole = [&](int st) {
       f32x16 s[NB];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) scores(nb * 32, st, s[nb]);
-      between();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         __builtin_amdgcn_sched_barrier(0);
@@ -217,75 +213,50 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int n_whole = min(max(lo_all - key0, 0) / BC, cnt);
 
     if constexpr (KIND != 1) {
-      int* entries = reinterpret_cast<int*>(smem_raw + L::kTiles) + wave * 4 * 64;
-      // table entries of tile j's rows, by way of LDS: an entry in a register would be waited for with every tile behind it.
-      // Rows behind the last repeat it and are masked.
-      auto fetch_entries = [&](int j) {
-        const int n = min(tile_at(j) + lane, hi_all - 1);
-        word_to_lds(table + min(divide(n, p.ps), pages - 1), entries + (j & 3) * 64);
-      };
-      // A wave takes BC / 4 consecutive rows of a tile: NK pieces of 1 KB of the keys, and as many of the values.  Where they come
-      // from, in 16-byte units behind the pools' starts (32 bits: 64 GiB).
+      // A wave takes BC / 4 consecutive rows of a tile: NK pieces of 1 KB of the keys, and as many of the values.  Rows that lie in
+      // one page (the usual sizes): its number comes by a scalar read, there is one start for the wave, in 16-byte units (32 bits:
+      // 64 GiB), and lanes add their row and chunk to it.  Rows behind the last are whatever the page holds, chunks behind a row's
+      // end (which meet zeros of the queries, or become channels that are not stored) repeat its last.  Else every lane looks up its
+      // own rows.
       constexpr int NK = BC * D / 512 / 4, ROWS = BC / 4;
       static_assert(ROWS == 16, "rows of a wave");
       const uint32_t k16 = (uint32_t)(p.k_stride / 8), v16 = (uint32_t)(p.v_stride / 8), rk = p.r3 / 8, rv = p.rt3 / 8;
-      auto row_of = [](int l, int i) { return i * RPP + l / CPR; };                                 // of the wave's
-      auto chunk_of = [](int l, int i) { return (l % CPR) ^ swz_x<CPR>(i * RPP + l / CPR); };
-      // Rows that lie in one page and fill the tile's width: one start for the wave, and what its lanes add to it.  Rows behind the
-      // last are whatever the page holds.
-      const bool straight = p.page_size % ROWS == 0 && first % ROWS == 0 && p.r3 == D && (KIND != 0 || p.rt3 == D);
-      // (in bytes, of its first piece; the others' differ in two bits of the chunk and in the row)
-      const uint32_t add0 = row_of(lane, 0) * (D * 2) + chunk_of(lane, 0) * 16;
-      static_assert(swz_x<CPR>(RPP) == (NK > 1 ? 4 : swz_x<CPR>(RPP)), "four chunks a piece");
-      uint32_t kstart = 0, vstart = 0;
-      auto find = [&](int j) {
-        const int n = tile_at(j) + wave * ROWS;
-        const uint32_t page = paged_page(__builtin_amdgcn_readfirstlane(entries[(j & 3) * 64 + wave * ROWS]), p.n_pages);
-        const uint32_t at = n - divide(n, p.ps) * p.page_size;
-        kstart = page * k16 + at * rk;
-        if constexpr (KIND == 0) vstart = page * v16 + at * rv;
-      };
-      auto issue = [&](int st) {
+      const bool straight = p.page_size % ROWS == 0 && first % ROWS == 0;
+      const auto* entries = (const __attribute__((address_space(4))) int*)table;
+      auto entry_at = [&](int j) { return entries[min(divide(min(tile_at(j) + wave * ROWS, hi_all - 1), p.ps), pages - 1)]; };
+      int entry = entry_at(0);                                    // of the tile that is filled next
+      auto fill = [&](int j, int st) {
         T* kt = smem + (long)st * L::kStage + wave * NK * 512;
-        const char *k = static_cast<const char*>(p.K) + (unsigned long)kstart * 16, *v = static_cast<const char*>(p.V) + (unsigned long)vstart * 16;
+        const int n0 = tile_at(j) + wave * ROWS;
+        int l = lane;
+        asm volatile("" : "+v"(l));                               // (chunks of the pieces are formed afresh, not kept across the loop)
+        if (straight) {
+          const uint32_t page = paged_page(entry, p.n_pages), at = n0 - divide(n0, p.ps) * p.page_size;
+          const char* k = static_cast<const char*>(p.K) + (unsigned long)(page * k16 + at * rk) * 16;
+          const char* v = KIND == 0 ? static_cast<const char*>(p.V) + (unsigned long)(page * v16 + at * rv) * 16 : nullptr;
 #pragma unroll
-        for (int i = 0; i < NK; ++i) {
-          const uint32_t add = (add0 ^ (64 * i)) + i * 1024;
-          chunk_to_lds(k + add, kt + i * 512);
-          if constexpr (KIND == 0) chunk_to_lds(v + add, kt + L::kTile + i * 512);
-        }
-      };
-      // Else every lane looks up its own row (those behind the last repeat it; chunks behind a row's end are zeros)
-      auto find_and_issue = [&](int j, int st) {
-        const int* ids = entries + (j & 3) * 64 + wave * ROWS;
-        T* kt = smem + (long)st * L::kStage + wave * NK * 512;
+          for (int i = 0; i < NK; ++i) {
+            const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(i * RPP + l / CPR);
+            chunk_to_lds(k + (row * rk + min(c, rk - 1)) * 16, kt + i * 512);
+            if constexpr (KIND == 0) chunk_to_lds(v + (row * rv + min(c, rv - 1)) * 16, kt + L::kTile + i * 512);
+          }
+          entry = entry_at(j + 1);
+        } else {
 #pragma unroll 1
-        for (int i = 0; i < NK; ++i) {
-          const uint32_t c = chunk_of(lane, i);
-          const int n = min(tile_at(j) + wave * ROWS + row_of(lane, i), hi_all - 1);
-          const uint32_t page = paged_page(ids[row_of(lane, i)], p.n_pages), at = n - divide(n, p.ps) * p.page_size;
-          const u32x4* k = static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + c);
-          chunk_to_lds(c < rk ? k : paged_zeros, kt + i * 512);
-          if constexpr (KIND == 0) {
-            const u32x4* v = static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + c);
-            chunk_to_lds(c < rv ? v : paged_zeros, kt + L::kTile + i * 512);
+          for (int i = 0; i < NK; ++i) {
+            const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(row);
+            const int n = min(n0 + (int)row, hi_all - 1), in_table = divide(n, p.ps);
+            const uint32_t page = paged_page(table[min(in_table, pages - 1)], p.n_pages), at = n - in_table * p.page_size;
+            chunk_to_lds(static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + min(c, rk - 1)), kt + i * 512);
+            if constexpr (KIND == 0)
+              chunk_to_lds(static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + min(c, rv - 1)), kt + L::kTile + i * 512);
           }
         }
       };
-      fetch_entries(0);
-      fetch_entries(1);
-      fetch_entries(2);
-      wait_vm<0>();                                               // entries, and plain loads out of the way of the counted ones
-      auto fill = [&](int j, int st) {
-        if (straight) issue(st);
-        else find_and_issue(j, st);
-        fetch_entries(j + 3);
-      };
-      if (straight) find(0);
+      wait_vm<0>();                                               // plain loads out of the way of the counted ones
       fill(0, 0);
-      if (straight) find(1);
       auto arrived = [] {
-        wait_vm<1>();                                             // this wave's part of tile j is there (entries may be on their way),
+        wait_vm<0>();                                             // this wave's part of tile j is there,
         wait_lds();                                               // its reads of tile j - 1 are done
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -294,11 +265,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (; j < n_whole; ++j) {
         arrived();
         fill(j + 1, (j + 1) & 1);                                 // into the stage of tile j - 1
-        whole(j & 1, [&] { if (straight) find(j + 2); });
+        whole(j & 1);
       }
       for (; j < cnt; ++j) {
         arrived();
-        if (straight) find(j + 1);
         fill(j + 1, (j + 1) & 1);
         edge(j, j & 1);
       }
@@ -354,7 +324,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         __syncthreads();
         store((j + 1) & 1);                                       // the stage of tile j - 1
         load(j + 2);
-        whole(j & 1, [] {});
+        whole(j & 1);
       }
       for (; j < cnt; ++j) {                                      // (nothing is kept in registers for later: they are all in use)
         __syncthreads();
