@@ -72,6 +72,20 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
   const int t = (int)min(item / parts, (long)p.T), part = (int)(item % parts);
   const bool live = slot < slots && t < p.T;
 
+  // the rows are on their way while the token's sequence is looked for
+  const int c = ch * N, h0 = part * kAppendHeads;
+  const bool queries = part < parts - 1;
+  const long qrow = ((long)t * p.nH + h0) * p.q_row + c;
+  Row16<T> r[kAppendHeads];
+  if (live && queries && c < p.r3) {
+#pragma unroll
+    for (int i = 0; i < kAppendHeads; ++i)
+      if (h0 + i < p.nH) load16<T, WIDE>(static_cast<const T*>(p.Qin) + qrow + (long)i * p.q_row, r[i]);
+  } else if (live && !queries) {
+    if (c < p.r3) load16<T, WIDE>(static_cast<const T*>(p.Kin) + t * p.ldk + c, r[0]);
+    if (p.V != nullptr && c < p.rt3) load16<T, WIDE>(static_cast<const T*>(p.Vin) + t * p.ldv + c, r[1]);
+  }
+
   // sequence of the token: as many of q_start[1 ..] as are not behind it
   int b = 0;
   for (int at = 1; at <= p.B; at += kAppendStarts) {
@@ -92,7 +106,6 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
   const PagedSeq s = paged_seq(p, b);
   if (t < s.q0 || t >= s.q0 + s.nq) return;
   const int pos = s.len - s.nq + (t - s.q0);                      // negative: before the sequence's first row
-  const int c = ch * N;
 
   f32x4 cs[N / 4];
 #pragma unroll
@@ -102,16 +115,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
 #pragma unroll
     for (int q = 0; q < N / 4; ++q) cs[q] = tab[(long)q * p.rope_ld];
   }
-  if (part < parts - 1) {                                         // ---- query rows
-    const int h0 = part * kAppendHeads;
-    const long row = ((long)t * p.nH + h0) * p.q_row + c;
+  if (queries) {
     if (c >= p.r3) return;
-    const T* src = static_cast<const T*>(p.Qin) + row;
-    T* dst = static_cast<T*>(p.Qout) + row;
-    Row16<T> r[kAppendHeads];
-#pragma unroll
-    for (int i = 0; i < kAppendHeads; ++i)
-      if (h0 + i < p.nH) load16<T, WIDE>(src + (long)i * p.q_row, r[i]);
+    T* dst = static_cast<T*>(p.Qout) + qrow;
 #pragma unroll
     for (int i = 0; i < kAppendHeads; ++i)
       if (h0 + i < p.nH) {
@@ -126,16 +132,11 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
   const int page = p.table[(long)b * p.max_pages + i];
   if ((uint32_t)page >= (uint32_t)p.n_pages) return;              // no page: nothing is stored
   const int at = pos - i * p.page_size;
-  Row16<T> r;
   if (c < p.r3) {
-    load16<T, WIDE>(static_cast<const T*>(p.Kin) + t * p.ldk + c, r);
-    if (p.rope != nullptr && p.rotate_k) turn<T>(r, cs);
-    store16<T, true>(static_cast<T*>(p.K) + page * p.k_stride + (long)at * p.r3 + c, r);
+    if (p.rope != nullptr && p.rotate_k) turn<T>(r[0], cs);
+    store16<T, true>(static_cast<T*>(p.K) + page * p.k_stride + (long)at * p.r3 + c, r[0]);
   }
-  if (p.V != nullptr && c < p.rt3) {
-    load16<T, WIDE>(static_cast<const T*>(p.Vin) + t * p.ldv + c, r);
-    store16<T, true>(static_cast<T*>(p.V) + page * p.v_stride + (long)at * p.rt3 + c, r);
-  }
+  if (p.V != nullptr && c < p.rt3) store16<T, true>(static_cast<T*>(p.V) + page * p.v_stride + (long)at * p.rt3 + c, r[1]);
 }
 
 template <typename T> static hipError_t append_one(const PagedAppendArgs& a, hipStream_t s) {
