@@ -238,7 +238,7 @@ int tucker_attn_backward(tucker_attn_ctx *ctx, const tucker_attn_weights *w,
  * Weights that stay fixed over many calls (serving): prepare their operand-layout copies once
  * (the head-mixed cores G_i = sum_a U1[i,a] C[a] of Section "KV Caching" and the transposed, padded
  * factor matrices, step one of every forward / decode call) into a caller-owned device buffer, and
- * every later forward / decode / backward call of this context skips that step.
+ * every later forward / decode / backward call (over pages too) of this context skips that step.
  *   prepared   device, >= tucker_attn_prepared_weights_bytes(ctx) bytes, 256-byte aligned
  * Exception to the ownership rule above: the context keeps the pointer `prepared` and the eight
  * weight pointers of `w` until tucker_attn_release_weights or tucker_attn_destroy; the caller keeps
@@ -331,6 +331,21 @@ int tucker_attn_attend_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *page
 int tucker_attn_attend_prefix(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
                               const int32_t *prefix_table, int32_t prefix_len, const void *Q, void *O, float *lse,
                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The whole layer over a paged cache: tucker_attn_forward for the T token rows of a step whose sequences live in pages.  Their
+ * latents are made and appended, the attention reads the pages (a common prefix once), the heads are merged:
+ *   X   device [T, d_model]   in: the tokens of all sequences, one sequence behind the other (q_start)
+ *   Y   device [T, d_model]   out, storage type; rows of X behind the last sequence leave rows of Y that mean nothing
+ * Serves prompts, pieces of prompts, proposed and single tokens, any mixture of them in one step.  prefix_table may be NULL with
+ * prefix_len 0; the prefix's rows are appended beforehand, by a call without one.  Differs from forward and decode in that the
+ * per-head queries and outputs pass through memory in the storage type (bf16: two more roundings).
+ * Limits and refusals: those of append and attend above, and 65535 * 32 tokens.
+ */
+size_t tucker_attn_forward_paged_workspace_bytes(const tucker_attn_ctx *ctx, const tucker_attn_batch *batch, int32_t prefix_len);
+int tucker_attn_forward_paged(tucker_attn_ctx *ctx, const tucker_attn_weights *w, const void *X, void *Y,
+                              const tucker_attn_pages *pages, const tucker_attn_batch *batch, const int32_t *prefix_table,
+                              int32_t prefix_len, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Optional per-kernel timing for benchmarks.  While enabled, forward/backward/decode bracket every

@@ -24,6 +24,7 @@ EXPORTED = [
     "tucker_attn_backward_workspace_bytes", "tucker_attn_backward",
     "tucker_attn_prepared_weights_bytes", "tucker_attn_prepare_weights", "tucker_attn_release_weights",
     "tucker_attn_append_paged", "tucker_attn_attend_workspace_bytes", "tucker_attn_attend_paged", "tucker_attn_attend_prefix",
+    "tucker_attn_forward_paged_workspace_bytes", "tucker_attn_forward_paged",
     "tucker_attn_profile_enable", "tucker_attn_profile_read", "tucker_attn_measure_mfma_ceiling",
     "tucker_attn_status_string",
 ]
@@ -171,6 +172,11 @@ def load_library() -> C.CDLL:
     lib.tucker_attn_attend_prefix.argtypes = [ctx_p, pages_p, batch_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                               C.c_void_p, C.c_size_t, C.c_void_p]
     lib.tucker_attn_attend_prefix.restype = C.c_int
+    lib.tucker_attn_forward_paged_workspace_bytes.argtypes = [ctx_p, batch_p, C.c_int32]
+    lib.tucker_attn_forward_paged_workspace_bytes.restype = C.c_size_t
+    lib.tucker_attn_forward_paged.argtypes = [ctx_p, C.POINTER(tucker_attn_weights), C.c_void_p, C.c_void_p, pages_p, batch_p,
+                                              C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.tucker_attn_forward_paged.restype = C.c_int
     lib.tucker_attn_profile_enable.argtypes = [ctx_p, C.c_int32]
     lib.tucker_attn_profile_enable.restype = C.c_int
     lib.tucker_attn_profile_read.argtypes = [ctx_p, C.POINTER(C.c_char_p), C.POINTER(C.c_float), C.c_int32]
@@ -395,17 +401,43 @@ def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_a
     return st
 
 
+def _prefix(pages, prefix_table, prefix_len) -> None:
+    if prefix_len > 0 and prefix_table is not None and (str(prefix_table.dtype) != "torch.int32" or not prefix_table.is_contiguous() or
+                                                        prefix_table.numel() * pages.page_size < prefix_len):
+        raise TuckerAttnError("prefix_table: int32, a page for every page_size rows of the prefix")
+
+
 def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, prefix_table, prefix_len: int, Q, O,
                               lse=None, workspace=None, stream=None, check: bool = True) -> int:
     """tucker_attn_attend_paged behind a common prefix; prefix_table: int32 device tensor with the pages of its rows."""
     _attend_rows(pages, batch, Q, O, lse)
-    if prefix_len > 0 and (str(prefix_table.dtype) != "torch.int32" or prefix_table.numel() * pages.page_size < prefix_len):
-        raise TuckerAttnError("prefix_table: int32, a page for every page_size rows of the prefix")
+    _prefix(pages, prefix_table, prefix_len)
     st = load_library().tucker_attn_attend_prefix(ctx, C.byref(pages), C.byref(batch), _ptr(prefix_table), int(prefix_len),
                                                   Q.data_ptr(), O.data_ptr(), _ptr(lse), _ptr(workspace),
                                                   0 if workspace is None else workspace.numel(), _stream_ptr(stream))
     if check:
         _check(st, "tucker_attn_attend_prefix")
+    return st
+
+
+def tucker_attn_forward_paged_workspace_bytes(ctx: int, batch: tucker_attn_batch, prefix_len: int = 0) -> int:
+    return int(load_library().tucker_attn_forward_paged_workspace_bytes(ctx, C.byref(batch), int(prefix_len)))
+
+
+def tucker_attn_forward_paged(ctx: int, weights: Dict, X, Y, pages: tucker_attn_pages, batch: tucker_attn_batch, prefix_table=None,
+                              prefix_len: int = 0, workspace=None, stream=None, check: bool = True) -> int:
+    """X, Y: contiguous [T, d_model], the tokens of all sequences one sequence behind the other; weights: dict of contiguous device
+    tensors; workspace: device uint8 tensor of at least tucker_attn_forward_paged_workspace_bytes bytes."""
+    for t in (X, Y):
+        if t.dim() != 2 or t.shape[0] != batch.T or t.shape != X.shape or t.dtype != pages.dtype or not t.is_contiguous():
+            raise TuckerAttnError(f"X, Y: {tuple(t.shape)} {t.dtype} where {batch.T} contiguous rows of {pages.dtype} are expected")
+    _prefix(pages, prefix_table, prefix_len)
+    ws = _weights_struct(weights)
+    st = load_library().tucker_attn_forward_paged(ctx, C.byref(ws), X.data_ptr(), Y.data_ptr(), C.byref(pages), C.byref(batch),
+                                                  _ptr(prefix_table), int(prefix_len), _ptr(workspace),
+                                                  0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+    if check:
+        _check(st, "tucker_attn_forward_paged")
     return st
 
 

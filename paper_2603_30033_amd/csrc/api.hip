@@ -12,7 +12,6 @@ using namespace ta;
 namespace {
 // Token tiles (32 padded tokens at the smallest) are the y dimension of the GEMM launches, which HIP
 // limits to 65535: more padded tokens than this are refused before anything is enqueued.
-constexpr long kMaxTokens = 65535l * 32;
 constexpr int kDecodeChunk = 32;      // sequences per pass of the decode kernels (their per-sequence arguments)
 }  // namespace
 
@@ -58,6 +57,7 @@ size_t prepared_bytes(const tucker_attn_ctx* c) {
   Carver cv{nullptr, 0};
   void *a, *b, *d, *e;
   carve_weights(c, cv, a, b, d, e);
+  (void)carve_query_core(c, cv);
   return cv.off;
 }
 
@@ -258,12 +258,7 @@ int forward_core(tucker_attn_ctx* c, const tucker_attn_weights* w, const void* X
   if (rec.on) c->kev_name = "attention_kernel";
   rec.after("attention");
 
-  GemmArgs z;
-  std::memset(&z, 0, sizeof(z));
-  z.A = ws.Gtil2; z.lda = (long)f.n_heads * c->D; z.M = c->RT2;
-  z.Bsrc = ws.O; z.ldb = (long)f.n_heads * c->D; z.K = f.n_heads * c->D;
-  z.Bsz = B; z.N = N; z.Npad = Npad; z.src_padded = 1;
-  z.epi = 1; z.Out = ws.Z; z.ldo = c->RT2; z.ksplit = 1; z.R2 = 0; z.D = 0;
+  const GemmArgs z = merge_product(c, ws.Gtil2, ws.O, ws.Z, B, N, Npad);
   if (launch_gemm(f.dtype, z, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   rec.after("latent_merge");
   return TUCKER_ATTN_OK;
@@ -521,15 +516,7 @@ int tucker_attn_forward(tucker_attn_ctx* c, const tucker_attn_weights* w, const 
       st != TUCKER_ATTN_OK)
     return st;
 
-  GemmArgs y;
-  std::memset(&y, 0, sizeof(y));
-  y.A = ut2; y.lda = ut2_ld; y.M = f.d_model;
-  y.Bsrc = ws.Z; y.ldb = c->RT2; y.K = c->RT2;
-  y.Bsz = B; y.N = N; y.Npad = Npad; y.src_padded = 1;
-  y.epi = 2; y.Out = Y; y.ldo = f.d_model; y.ksplit = 1;
-  const hipError_t ye = out_proj_supported(f.dtype, y) ? launch_out_proj(f.dtype, y, s)
-                                                       : launch_gemm(f.dtype, y, s);
-  if (ye != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (launch_output(c, ut2, ut2_ld, ws.Z, Y, B, N, Npad, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   rec.after("output_projection");
   return TUCKER_ATTN_OK;
 }
@@ -731,9 +718,10 @@ int tucker_attn_prepare_weights(tucker_attn_ctx* c, const tucker_attn_weights* w
   Carver cv{static_cast<char*>(prepared), 0};
   void *Gt, *Gtil2, *Wcat, *Ut2p;
   carve_weights(c, cv, Gt, Gtil2, Wcat, Ut2p);
+  void* Gq = carve_query_core(c, cv);
   const void* ut2;
   long ut2_ld;
-  PrepArgs pa = make_prep(c, w, Gt, Gtil2, Wcat, Ut2p, &ut2, &ut2_ld);
+  PrepArgs pa = make_prep(c, w, Gt, Gtil2, Wcat, Ut2p, &ut2, &ut2_ld, true, Gq);
   if (launch_prep(c->cfg.dtype, pa, static_cast<hipStream_t>(hip_stream)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   c->prepared = prepared;
   c->prepared_from = *w;

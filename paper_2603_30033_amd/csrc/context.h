@@ -12,6 +12,7 @@
 namespace ta {
 constexpr int kMaxKernels = 40;
 constexpr size_t kAlign = 256;
+constexpr long kMaxTokens = 65535l * 32;   // token rows of a call (32-row tiles along a grid dimension)
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 }  // namespace ta
 
@@ -55,6 +56,12 @@ inline void carve_weights(const tucker_attn_ctx* c, Carver& cv, void*& Gt, void*
   Ut2p = cv.take<char>((size_t)c->dp * c->RT2 * c->es);
 }
 
+// Head-mixed query core as rows [n_heads * D][R2]: the calls over pages keep their queries in memory and make them with one
+// product.  Behind carve_weights in a prepared buffer.
+inline void* carve_query_core(const tucker_attn_ctx* c, Carver& cv) {
+  return cv.take<char>((size_t)c->cfg.n_heads * c->D * c->R2 * c->es);
+}
+
 // The operand-layout copies of the weights: a piece of the call's workspace, or the caller's
 // prepared buffer when one is registered (then no preparation kernel runs).
 template <typename W> inline void use_prepared(const tucker_attn_ctx* c, W& w) {
@@ -80,16 +87,19 @@ inline void add_job(PrepArgs& pa, const void* src, const void* coef, void* out, 
   pa.total_blocks += prep_job_blocks(j);
 }
 
-// head-mixed cores and factor matrices in MFMA operand layout; returns the output-factor pointer
+// head-mixed cores (Gt or Gq null: not that one) and factor matrices in MFMA operand layout; returns the output-factor pointer
 inline PrepArgs make_prep(const tucker_attn_ctx* c, const tucker_attn_weights* w, void* Gt, void* Gtil2, void* Wcat,
-                   void* Ut2p, const void** ut2_used, long* ut2_ld, bool with_wcat = true) {
+                   void* Ut2p, const void** ut2_used, long* ut2_ld, bool with_wcat = true, void* Gq = nullptr) {
   const tucker_attn_config& f = c->cfg;
   const int es = c->es;
   PrepArgs pa;
   std::memset(&pa, 0, sizeof(pa));
   const long nHD = (long)f.n_heads * c->D;
   // Gt[i][c][b] = qscale * sum_a U1[i,a] C[a,b,c], fragment-major 32x32 blocks of (c, b)
-  add_job(pa, w->C, w->U1, Gt, f.r1, f.r2, f.r3, f.n_heads, c->R2, c->D, (long)c->D * c->R2, c->R2, 1, 1, c->qscale, 1);
+  if (Gt)
+    add_job(pa, w->C, w->U1, Gt, f.r1, f.r2, f.r3, f.n_heads, c->R2, c->D, (long)c->D * c->R2, c->R2, 1, 1, c->qscale, 1);
+  // Gq[i*D + c][b] = sum_a U1[i,a] C[a,b,c], b in acc order like the query latents
+  if (Gq) add_job(pa, w->C, w->U1, Gq, f.r1, f.r2, f.r3, f.n_heads, c->R2, c->D, (long)c->D * c->R2, c->R2, 1, 1, 1.f);
   // Gtil2[b][i*D + c] = sum_a U~1[i,a] C~[a,b,c]
   add_job(pa, w->Ct, w->Ut1, Gtil2, f.rt1, f.rt2, f.rt3, f.n_heads, c->RT2, c->D, c->D, nHD, 0, 1, 1.f);
   // Wcat rows: U2^T | U3^T | U~3^T, each [rank_pad][dp]
@@ -128,6 +138,27 @@ struct Recorder {
     return hipEventRecord(c->ev[c->n_kernels], s);
   }
 };
+
+// Z = O Gtil2^T (latent merge of the heads) and Y = Z U~2^T, over B x Npad token rows of which N of every Npad exist
+inline GemmArgs merge_product(const tucker_attn_ctx* c, const void* Gtil2, const void* O, void* Z, int B, int N, int Npad) {
+  GemmArgs z;
+  std::memset(&z, 0, sizeof(z));
+  z.A = Gtil2; z.lda = (long)c->cfg.n_heads * c->D; z.M = c->RT2;
+  z.Bsrc = O; z.ldb = (long)c->cfg.n_heads * c->D; z.K = c->cfg.n_heads * c->D;
+  z.Bsz = B; z.N = N; z.Npad = Npad; z.src_padded = 1;
+  z.epi = 1; z.Out = Z; z.ldo = c->RT2; z.ksplit = 1; z.R2 = 0; z.D = 0;
+  return z;
+}
+inline hipError_t launch_output(const tucker_attn_ctx* c, const void* ut2, long ut2_ld, const void* Z, void* Y, int B, int N, int Npad,
+                                hipStream_t s) {
+  GemmArgs y;
+  std::memset(&y, 0, sizeof(y));
+  y.A = ut2; y.lda = ut2_ld; y.M = c->cfg.d_model;
+  y.Bsrc = Z; y.ldb = c->RT2; y.K = c->RT2;
+  y.Bsz = B; y.N = N; y.Npad = Npad; y.src_padded = 1;
+  y.epi = 2; y.Out = Y; y.ldo = c->cfg.d_model; y.ksplit = 1;
+  return out_proj_supported(c->cfg.dtype, y) ? launch_out_proj(c->cfg.dtype, y, s) : launch_gemm(c->cfg.dtype, y, s);
+}
 
 inline bool weights_ok(const tucker_attn_ctx* c, const tucker_attn_weights* w) {
   return c && w && w->C && w->U1 && w->U2 && w->U3 && w->Ct && w->Ut1 && w->Ut2 && (w->Ut3 || c->cfg.shared_kv);

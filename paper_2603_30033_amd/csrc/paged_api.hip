@@ -98,29 +98,24 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   return cv.off;
 }
 
-int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const int32_t* prefix_table,
-           int32_t prefix, const void* Q, void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (int st = check_batch(c, batch)) return st;
-  if (int st = check_pool(c, pages, batch)) return st;
-  if (!Q || !O || !aligned16(Q) || !aligned16(O) || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return TUCKER_ATTN_INVALID_ARG;
-  if (prefix < 0 || prefix > batch->max_len || (prefix > 0 && !prefix_table)) return TUCKER_ATTN_INVALID_ARG;
-  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return TUCKER_ATTN_INVALID_ARG;
+int check_prefix(const tucker_attn_batch* b, const int32_t* table, int32_t prefix) {
+  return prefix < 0 || prefix > b->max_len || (prefix > 0 && !table) ? TUCKER_ATTN_INVALID_ARG : TUCKER_ATTN_OK;
+}
+
+// arguments of the attention over checked pages; returns the bytes of workspace it needs
+size_t attend_args(PagedArgs& a, const tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch,
+                   const int32_t* prefix_table, int32_t prefix, void* workspace) {
   const tucker_attn_config& f = c->cfg;
-  PagedArgs a;
   std::memset(&a, 0, sizeof(a));
   fill(a, c, pages, batch);
-  a.prefix_table = prefix_table;
-  a.Q = Q; a.O = O; a.lse = lse; a.q_row = f.r3; a.o_row = f.rt3;
+  a.prefix_table = prefix_table; a.q_row = f.r3; a.o_row = f.rt3;
   a.heads = divisor(f.n_heads); a.scale = c->qscale; a.causal = f.causal; a.shared_kv = f.shared_kv;
-  const size_t need = plan(c, batch, prefix, workspace, a);
-  if (need > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
-  if (workspace_bytes < need) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
+  return plan(c, batch, prefix, workspace, a);
+}
 
-  hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  Recorder rec{c, s, c->profile != 0};
-  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
-  const bool tile = f.dtype == TUCKER_ATTN_BF16;
-  if (prefix > 0) {
+int launch_attend(const tucker_attn_ctx* c, const PagedArgs& a, hipStream_t s, Recorder& rec) {
+  const bool tile = c->cfg.dtype == TUCKER_ATTN_BF16;
+  if (a.prefix > 0) {
     if ((tile ? launch_paged_tile(a, true, s) : launch_paged_rows(a, true, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("prefix_attention");
   }
@@ -133,6 +128,48 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
     (void)rec.after("paged_merge");
   }
   return TUCKER_ATTN_OK;
+}
+
+int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const int32_t* prefix_table,
+           int32_t prefix, const void* Q, void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (int st = check_batch(c, batch)) return st;
+  if (int st = check_pool(c, pages, batch)) return st;
+  if (!Q || !O || !aligned16(Q) || !aligned16(O) || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return TUCKER_ATTN_INVALID_ARG;
+  if (int st = check_prefix(batch, prefix_table, prefix)) return st;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return TUCKER_ATTN_INVALID_ARG;
+  PagedArgs a;
+  const size_t need = attend_args(a, c, pages, batch, prefix_table, prefix, workspace);
+  a.Q = Q; a.O = O; a.lse = lse;
+  if (need > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
+  if (workspace_bytes < need) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  Recorder rec{c, s, c->profile != 0};
+  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  return launch_attend(c, a, s, rec);
+}
+
+// Workspace of the layer over pages: operand copies of the weights, the tokens' latents, per-head queries and outputs (rows of D
+// channels, the outputs' in acc order), merged latents; behind them that of the attention.
+struct LayerWs {
+  void *Gt, *Gtil2, *Wcat, *Ut2p, *Gq, *Qlat, *K, *V, *Q, *O, *Z;
+  size_t bytes;
+};
+LayerWs carve_layer(const tucker_attn_ctx* c, void* ws, long T) {
+  const tucker_attn_config& f = c->cfg;
+  const size_t es = c->es, heads = (size_t)T * f.n_heads * c->D * es;
+  Carver cv{static_cast<char*>(ws), 0};
+  LayerWs w;
+  carve_weights(c, cv, w.Gt, w.Gtil2, w.Wcat, w.Ut2p);
+  w.Gq = w.Gt;                                                    // the same size, and this one is not needed
+  w.Gt = nullptr;
+  w.Qlat = cv.take<char>(T * c->R2 * es);
+  w.K = cv.take<char>(T * f.r3 * es);
+  w.V = cv.take<char>(f.shared_kv ? 0 : T * f.rt3 * es);
+  w.Q = cv.take<char>(heads);
+  w.O = cv.take<char>(heads);
+  w.Z = cv.take<char>(T * c->RT2 * es);
+  w.bytes = cv.off;
+  return w;
 }
 
 }  // namespace
@@ -179,6 +216,86 @@ int tucker_attn_attend_prefix(tucker_attn_ctx* c, const tucker_attn_pages* pages
                               const int32_t* prefix_table, int32_t prefix_len, const void* Q, void* O, float* lse,
                               void* workspace, size_t workspace_bytes, void* hip_stream) {
   return attend(c, pages, batch, prefix_table, prefix_len, Q, O, lse, workspace, workspace_bytes, hip_stream);
+}
+
+size_t tucker_attn_forward_paged_workspace_bytes(const tucker_attn_ctx* c, const tucker_attn_batch* batch, int32_t prefix_len) {
+  if (check_batch(c, batch) != TUCKER_ATTN_OK || prefix_len < 0 || prefix_len > batch->max_len || batch->T > kMaxTokens) return 0;
+  PagedArgs a;
+  return carve_layer(c, nullptr, batch->T).bytes + plan(c, batch, prefix_len, nullptr, a);
+}
+
+int tucker_attn_forward_paged(tucker_attn_ctx* c, const tucker_attn_weights* w, const void* X, void* Y, const tucker_attn_pages* pages,
+                              const tucker_attn_batch* batch, const int32_t* prefix_table, int32_t prefix_len, void* workspace,
+                              size_t workspace_bytes, void* hip_stream) {
+  if (int st = check_batch(c, batch)) return st;
+  if (int st = check_pool(c, pages, batch)) return st;
+  if (!weights_ok(c, w) || !X || !Y || !workspace) return TUCKER_ATTN_INVALID_ARG;
+  if (int st = check_prefix(batch, prefix_table, prefix_len)) return st;
+  if (batch->T > kMaxTokens) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return TUCKER_ATTN_INVALID_ARG;
+  if (c->prepared && !same_weights(*w, c->prepared_from)) return TUCKER_ATTN_INVALID_ARG;
+  const tucker_attn_config& f = c->cfg;
+  const int T = batch->T;
+  LayerWs ws = carve_layer(c, workspace, T);
+  PagedArgs a;
+  const size_t attend_bytes = attend_args(a, c, pages, batch, prefix_table, prefix_len, static_cast<char*>(workspace) + ws.bytes);
+  if (workspace_bytes < ws.bytes + attend_bytes) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
+
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  Recorder rec{c, s, c->profile != 0};
+  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (c->prepared) {
+    Carver cv{static_cast<char*>(c->prepared), 0};
+    carve_weights(c, cv, ws.Gt, ws.Gtil2, ws.Wcat, ws.Ut2p);
+    ws.Gq = carve_query_core(c, cv);
+  }
+  const void* ut2;
+  long ut2_ld;
+  const PrepArgs pa = make_prep(c, w, nullptr, ws.Gtil2, ws.Wcat, ws.Ut2p, &ut2, &ut2_ld, true, ws.Gq);
+  if (!c->prepared) {
+    if (launch_prep(f.dtype, pa, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+    (void)rec.after("prep_weights");
+  }
+
+  // the tokens of all sequences are the rows of each product; their latents are not rotated here
+  GemmArgs g;
+  std::memset(&g, 0, sizeof(g));
+  g.A = ws.Wcat; g.lda = c->dp; g.M = c->R2 + (f.shared_kv ? 1 : 2) * c->D; g.shared_kv = f.shared_kv;
+  g.Bsrc = X; g.ldb = f.d_model; g.K = f.d_model;
+  g.Bsz = 1; g.N = T; g.Npad = T; g.src_padded = 1;
+  g.epi = 0;
+  g.Qlat = ws.Qlat; g.R2 = c->R2; g.D = c->D;
+  g.Kcache = ws.K; g.Vcache = f.shared_kv ? nullptr : ws.V; g.Lmax = T; g.r3 = f.r3; g.rt3 = f.rt3;
+  g.ksplit = 1;
+  if (launch_gemm(f.dtype, g, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("factor_projection");
+
+  GemmArgs q;
+  std::memset(&q, 0, sizeof(q));
+  q.A = ws.Gq; q.lda = c->R2; q.M = f.n_heads * c->D;
+  q.Bsrc = ws.Qlat; q.ldb = c->R2; q.K = c->R2;
+  q.Bsz = 1; q.N = T; q.Npad = T; q.src_padded = 1;
+  q.epi = 1; q.Out = ws.Q; q.ldo = q.M; q.ksplit = 1;
+  if (launch_gemm(f.dtype, q, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("head_queries");
+
+  PagedAppendArgs p;
+  std::memset(&p, 0, sizeof(p));
+  fill(p, c, pages, batch);
+  p.Kin = ws.K; p.ldk = f.r3; p.Vin = f.shared_kv ? nullptr : ws.V; p.ldv = f.rt3;
+  p.Qin = p.Qout = f.use_rope ? ws.Q : nullptr; p.q_row = c->D;   // (queries in place)
+  p.rotate_k = !f.shared_kv;
+  if (launch_paged_append(f.dtype, p, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("paged_append");
+
+  a.Q = ws.Q; a.q_row = c->D; a.O = ws.O; a.o_row = c->D; a.o_acc = 1;
+  if (int st = launch_attend(c, a, s, rec)) return st;
+
+  if (launch_gemm(f.dtype, merge_product(c, ws.Gtil2, ws.O, ws.Z, 1, T, T), s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("latent_merge");
+  if (launch_output(c, ut2, ut2_ld, ws.Z, Y, 1, T, T, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  (void)rec.after("output_projection");
+  return TUCKER_ATTN_OK;
 }
 
 }  // extern "C"

@@ -96,6 +96,15 @@ class Layer:
         ta.tucker_attn_decode(self.ctx, self.weights, x, y, Kc, Vc, [int(v) for v in kv_len], ws)
         return y
 
+    def forward_paged(self, X: torch.Tensor, pages, batch, prefix_table=None, prefix_len: int = 0, Y=None) -> torch.Tensor:
+        """One step of the sequences of `batch` (binding.tucker_attn_batch) whose cached rows live in `pages`
+        (binding.tucker_attn_pages): X, Y [T, d_model], the tokens of all sequences one sequence behind the other."""
+        if Y is None:
+            Y = torch.empty_like(X)
+        ws = self.workspace(ta.tucker_attn_forward_paged_workspace_bytes(self.ctx, batch, prefix_len))
+        ta.tucker_attn_forward_paged(self.ctx, self.weights, X, Y, pages, batch, prefix_table, prefix_len, ws)
+        return Y
+
 
 # ---- weight front-ends ---------------------------------------------------------------------------
 

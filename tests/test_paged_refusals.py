@@ -122,3 +122,25 @@ def test_the_binding_checks_shapes_and_types():
         ta.tucker_attn_attend_prefix(None, p, b, i32(1), 17, Q, O)
     with pytest.raises(ta.TuckerAttnError):
         ta.tucker_attn_append_paged(None, p, b, Q[:, 0], O[:, 0, :32])
+
+
+def test_arguments_of_the_layer(ctx):
+    lib = ta.load_library()
+    w = C.byref(ta.tucker_attn_weights(*[256] * 8))
+    p, b = C.byref(pages()), C.byref(batch())
+    need = ta.tucker_attn_forward_paged_workspace_bytes(ctx, batch(), 8)
+    assert need > ta.tucker_attn_attend_workspace_bytes(ctx, batch(), 8)
+    run = lambda w=w, x=256, y=256, p=p, b=b, table=256, prefix=8, ws=256, size=need, c=ctx: lib.tucker_attn_forward_paged(
+        c, w, x, y, p, b, table, prefix, ws, size, None)
+    for bad in [dict(w=None), dict(w=C.byref(ta.tucker_attn_weights(*[256] * 7, None))), dict(x=None), dict(y=None), dict(table=None),
+                dict(prefix=-1), dict(prefix=65), dict(ws=None), dict(ws=264), dict(c=None), dict(p=None), dict(b=None)]:
+        assert run(**bad) == -1, bad
+    for bad in BAD_POOLS:
+        assert run(p=C.byref(pages(**bad))) == -1, bad
+    for bad in BAD_BATCHES:
+        assert run(b=C.byref(batch(**bad))) == -1, bad
+    assert run(size=need - 1) == -3
+    assert run(b=C.byref(batch(T=65535 * 32 + 1)), size=1 << 60) == -2
+    assert ta.tucker_attn_forward_paged_workspace_bytes(ctx, batch(T=65535 * 32 + 1)) == 0
+    assert ta.tucker_attn_forward_paged_workspace_bytes(ctx, batch(B=0)) == 0
+    assert ta.tucker_attn_forward_paged_workspace_bytes(ctx, batch(), -1) == 0
