@@ -49,6 +49,11 @@ struct PagedArgs {
   // takes a sequence's `hb` blocks of 32 rows at once and gives no workgroup less than stream_least units, and of paged_tile.
   // Rows that several workgroups share leave partial results: [workgroups][hb * 32] rows, [2 * workgroups][kTileRows].
   int hb, stream_wgs, stream_least, tile_wgs;
+  // paged_tile: work of a key of a row block, 1 / (kTileUnit nH); [0]: number of shares, then for each, if its start is the first in
+  // a row block behind the block's own: first row of the block, its rows (0 otherwise), last share in it, whether the first share
+  // in it begins in an earlier block
+  double tile_per_key;
+  int4* tile_cuts;
   float* stream_o;
   float2* stream_ml;
 };
@@ -82,7 +87,8 @@ hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s
 hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16
 hipError_t launch_paged_join(const PagedArgs& a, hipStream_t s);     // of its partial results, and the prefix's
 hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // bf16
-constexpr int kTileRows = 128, kTileUnit = 64, kTileLeast = 4;   // rows of a workgroup of paged_tile, keys of a unit of its work, least units
+// rows of a workgroup of paged_tile, keys of a unit of its work, units that a row block costs besides, least units of a share
+constexpr int kTileRows = 128, kTileUnit = 64, kTileBlock = 3, kTileLeast = 4;
 hipError_t launch_paged_tile_join(const PagedArgs& a, hipStream_t s);
 hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s);   // fp32
 

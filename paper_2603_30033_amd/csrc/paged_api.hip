@@ -82,7 +82,8 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     }
   } else if (tile) {
     const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
-    if (units > kTileLeast && blocks * units < (1l << 31)) a.tile_wgs = 2 * c->n_cus;
+    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31)) a.tile_wgs = 2 * c->n_cus;
+    a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
     const int parts = key_parts(c, paged_rows_blocks(a, block), keys, 2, 128);
@@ -95,6 +96,7 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   a.part_ml = cv.take<float2>(parts * rows * 8);
   a.stream_o = cv.take<float>(shared * c->D * 4);
   a.stream_ml = cv.take<float2>(shared * 8);
+  a.tile_cuts = cv.take<int4>(a.tile_wgs * sizeof(int4));
   return cv.off;
 }
 

@@ -20,10 +20,32 @@ template <int D, int KIND> struct TileLds {
   static constexpr size_t kBytes = 2ul * kStage * sizeof(bf16);
 };
 
-// row blocks of sequence b, and units of keys of each of them (no key of its own: one, which leaves the rows' empty result).  Rows that
-// see fewer keys than the sequence has count alike.
-__device__ __forceinline__ int tile_blocks(const PagedArgs& p, int b) { return (paged_seq(p, b).nq * p.nH + kTileRows - 1) / kTileRows; }
-__device__ __forceinline__ int tile_units(const PagedArgs& p, int b) { return max(1, (paged_seq(p, b).len - p.prefix + kTileUnit - 1) / kTileUnit); }
+__device__ __forceinline__ int tile_blocks(const PagedArgs& p, const PagedSeq& s) { return (s.nq * p.nH + kTileRows - 1) / kTileRows; }
+// The work of a sequence's first i row blocks: kTileBlock for each, and one for every kTileUnit keys that its last row sees (in closed
+// form: a block more sees kTileRows / nH keys more; doubles hold these integers exactly).  Not decreasing, and at most
+// i (kTileBlock + units of the sequence's own keys), whatever its lengths are.  Two prompts of 4096 tokens, 32 heads of 128 channels:
+// 354 us, with kTileBlock 1, 6, 12: 471, 357, 374, with blocks that count alike 577.  Eight of 1024 tokens, 12 heads of 64: 44, 55,
+// 45, 46, 49.
+__device__ __forceinline__ int tile_work(const PagedArgs& p, const PagedSeq& s, int i) {
+  constexpr double R = kTileRows;
+  const int own = max(s.len - p.prefix, 0), seen = p.causal ? max(s.len - s.nq - p.prefix, 0) : own;
+  const double n = i, keys = n * seen * p.nH + (p.causal ? R / 2 * n * (n + 1) : 0.);   // times nH
+  return i * kTileBlock + min((int)fmin(keys * p.tile_per_key, 2147483647.), i * ((own + kTileUnit - 1) / kTileUnit));
+}
+// the row block in which item `at` of the sequence's work lies
+__device__ __forceinline__ int tile_block(const PagedArgs& p, const PagedSeq& s, int at) {
+  int lo = 0, hi = tile_blocks(p, s);                             // work(lo) <= at < work(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (tile_work(p, s, mid) <= at) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__device__ __forceinline__ int tile_work(const PagedArgs& p, int b) {
+  const PagedSeq s = paged_seq(p, b);
+  return tile_work(p, s, tile_blocks(p, s));
+}
 
 template <int D, int KIND, bool PREFIX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tile_kernel(PagedArgs p) {
@@ -40,34 +62,49 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // Workgroups go to the eight dies in turn, and each die has a cache of its own: workgroup i of a die takes piece i of the die's
   // share of consecutive pieces, which read the same keys.
   const int die = blockIdx.x % 8, in_die = blockIdx.x / 8;
-  int b = 0, rb, unit = 0, left = 1, units_b = 1, part = 0, me = 0;   // sequence, row block, unit of its keys, units to do, units of a block
+  // sequence, row block, items of its work that others do before, all its items, items to do
+  int b = 0, rb, item = 0, items = 1, left = 1, part = 0, me = 0;
   if constexpr (PREFIX) {
     const int blocks = (p.T * p.nH + RB - 1) / RB, per = (blocks * p.prefix_parts + 7) / 8, piece = die * per + in_die;
     if (in_die >= per || piece >= blocks * p.prefix_parts) return;
     part = piece / blocks;
     rb = piece % blocks;
   } else {
-    int index, units;
+    int index, all;
     if (p.tile_wgs == 0) {                                        // a workgroup for every row block
-      b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, i); }, reinterpret_cast<int*>(smem_raw), rb, units);
+      b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
       if (b < 0) return;
-      left = units_b = tile_units(p, b);
     } else {
-      auto all = [&](int i) { return tile_blocks(p, i) * tile_units(p, i); };
-      b = paged_locate(p.B, 0, all, reinterpret_cast<int*>(smem_raw), index, units);
-      if (b < 0) return;
-      const Shares sh(units, p.tile_wgs, kTileLeast);
+      auto work = [&](int i) { return tile_work(p, i); };
+      b = paged_locate(p.B, 0, work, reinterpret_cast<int*>(smem_raw), index, all);
+      if (b < 0) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.tile_cuts[0].x = 0;
+        return;
+      }
+      const Shares sh(all, p.tile_wgs, kTileLeast);
       const int per = (sh.G + 7) / 8;
       me = die * per + in_die;
       if (in_die >= per || me >= sh.G) return;
-      left = sh.first(me + 1) - sh.first(me);
-      if (me > 0) b = paged_locate(p.B, sh.first(me), all, reinterpret_cast<int*>(smem_raw), index, units);
+      const int mine = sh.first(me);
+      left = sh.first(me + 1) - mine;
+      if (me > 0) b = paged_locate(p.B, mine, work, reinterpret_cast<int*>(smem_raw), index, all);
       b = __builtin_amdgcn_readfirstlane(b);
       index = __builtin_amdgcn_readfirstlane(index);
-      units_b = tile_units(p, b);
-      rb = index / units_b;
-      unit = index % units_b;
+      const PagedSeq s = paged_seq(p, b);
+      rb = tile_block(p, s, index);
+      item = index - tile_work(p, s, rb);
+      items = tile_work(p, s, rb + 1) - tile_work(p, s, rb);
+      if (threadIdx.x == 0) {                                     // for the join: how many shares there are, what starts in a block
+        const int at = mine - item;
+        if (me == 0) p.tile_cuts[0].x = sh.G;
+        else if (item == 0 || sh.group(at) != me - 1) p.tile_cuts[me].y = 0;   // at its start; behind another share's start
+        else
+          p.tile_cuts[me] = int4{s.q0 * p.nH + rb * RB, min(s.nq * p.nH - rb * RB, RB), sh.group(at + items - 1), sh.first(me - 1) < at};
+      }
     }
+    rb = __builtin_amdgcn_readfirstlane(rb);
+    item = __builtin_amdgcn_readfirstlane(item);
+    items = __builtin_amdgcn_readfirstlane(items);
   }
 
   for (int segment = 0; left > 0; ++segment) {
@@ -86,15 +123,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     table = p.table + (long)b * p.max_pages;
     pages = p.max_pages;
   }
-  const int n_rows = nq * p.nH, now = PREFIX ? 1 : min(left, units_b - unit);
+  const int n_rows = nq * p.nH, now = PREFIX ? 1 : min(left, items - item);
   const bool causal = !PREFIX && p.causal;
   const int r0 = rb * RB, rw = r0 + wave * 32;                 // first row of the workgroup, of this wave
   const int r = min(rw + lr, n_rows - 1);                         // rows behind the last repeat it and are not stored
   auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
   const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);     // keys that the row sees, that all and any rows of the workgroup see
   const int hi = sees(rw + 31);                                   // keys that any row of the wave sees
-  const int key0 = PREFIX ? part * p.prefix_keys : first + unit * kTileUnit;
-  const int key1 = min(hi_all, PREFIX ? key0 + p.prefix_keys : key0 + now * kTileUnit);
+  // items dealt to whole units of the keys that the block sees; who ends here and who goes on from here count alike
+  const int units = max(0, hi_all - first + kTileUnit - 1) / kTileUnit;
+  auto unit_at = [&](int i) { return i == 0 ? 0 : i == items ? units : __builtin_amdgcn_readfirstlane((int)((double)i * units / items)); };
+  const int key0 = PREFIX ? part * p.prefix_keys : first + unit_at(item) * kTileUnit;
+  const int key1 = min(hi_all, PREFIX ? key0 + p.prefix_keys : first + unit_at(item + now) * kTileUnit);
   const int cnt = key1 > key0 ? (key1 - key0 + BC - 1) / BC : 0;  // tiles
 
   f32x16 oacc[CB];
@@ -337,7 +377,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
   // ---- the rows: a result, or a part of one ----
   const float l = halves_sum(l_run);
-  const bool complete = !PREFIX && now == units_b;                // nobody else has keys of these rows
+  const bool complete = !PREFIX && now == items;                  // nobody else has keys of these rows
   if (rw + lr < n_rows) {
     const long at = (long)row0 + rw + lr;
     const bool direct = complete && p.prefix_parts == 0;
@@ -357,20 +397,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
   left -= now;
   if (PREFIX || left == 0) break;
-  unit = 0;
-  if (++rb == tile_blocks(p, b)) {
+  item = 0;
+  PagedSeq s = paged_seq(p, b);
+  if (++rb == tile_blocks(p, s)) {
     rb = 0;
-    do ++b;
-    while (tile_blocks(p, b) == 0);                               // (units are left, so a sequence with some follows)
-    units_b = tile_units(p, b);
+    do s = paged_seq(p, ++b);
+    while (s.nq == 0);                                            // (work is left, so a sequence with some follows)
   }
+  items = __builtin_amdgcn_readfirstlane(tile_work(p, s, rb + 1) - tile_work(p, s, rb));
   __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// The partial results of a row block: those of the prefix, and its own.  Grid: row blocks x groups of rows; a row by D/4 threads, or
-// by `groups` times as many.
+// The partial results of a row block: those of the prefix, and its own.  Grid: row blocks x groups of rows; without a prefix only
+// blocks that are shared have something to join, so the grid has the shares in place of the row blocks, and the workgroup that did
+// a share has left what there is to join at its start (to look for it here again: 20 us more).  A row by D/4 threads, or by `groups`
+// times as many.
 // ------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int groups) {
@@ -380,43 +423,50 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int g
   __shared__ float4 po[256];
   __shared__ float2 pml[SLOTS];
   const int tid = threadIdx.x, per = SLOTS / groups;
-  int rb, blocks, at_unit = 0, units = 1;
-  const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, i); }, sh, rb, blocks);
-  if (b < 0) return;
-  const PagedSeq s = paged_seq(p, b);
-  const int n_rows = min(s.nq * p.nH - rb * kTileRows, kTileRows);
-  if ((int)blockIdx.y * per >= n_rows) return;
-  int g0 = 0, g1 = 0;                                             // workgroups that share the block,
+  int n_rows, g0 = 0, g1 = 0;                                     // workgroups that share the block,
   bool cut = false;                                               // the first of them behind another block
-  if (p.tile_wgs > 0) {
-    int before = 0, all = 0;
-    for (int i = tid; i < p.B; i += 256) {
-      const int n = tile_blocks(p, i) * tile_units(p, i);
-      all += n;
-      if (i < b) before += n;
-    }
+  long row0;
+  if (p.prefix_parts > 0) {
+    int rb, all;
+    const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, sh, rb, all);
+    if (b < 0) return;
+    const PagedSeq s = paged_seq(p, b);
+    row0 = (long)s.q0 * p.nH + rb * kTileRows;
+    n_rows = min(s.nq * p.nH - rb * kTileRows, kTileRows);
+    if (p.tile_wgs > 0) {
+      int before = 0;
+      all = 0;
+      for (int i = tid; i < p.B; i += 256) {
+        const int n = tile_work(p, i);
+        all += n;
+        if (i < b) before += n;
+      }
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      all += __shfl_xor(all, d);
-      before += __shfl_xor(before, d);
+      for (int d = 1; d < kWave; d *= 2) {
+        all += __shfl_xor(all, d);
+        before += __shfl_xor(before, d);
+      }
+      if (tid % kWave == 0) {
+        sh[tid / kWave] = all;
+        sh[4 + tid / kWave] = before;
+      }
+      __syncthreads();
+      const int first = tile_work(p, s, rb), at = sh[4] + sh[5] + sh[6] + sh[7] + first;
+      const Shares share(sh[0] + sh[1] + sh[2] + sh[3], p.tile_wgs, kTileLeast);
+      g0 = share.group(at);
+      g1 = share.group(at + tile_work(p, s, rb + 1) - first - 1);
+      cut = share.first(g0) < at;
     }
-    if (tid % kWave == 0) {
-      sh[tid / kWave] = all;
-      sh[4 + tid / kWave] = before;
-    }
-    __syncthreads();
-    units = sh[0] + sh[1] + sh[2] + sh[3];
-    const int units_b = tile_units(p, b);
-    at_unit = sh[4] + sh[5] + sh[6] + sh[7] + rb * units_b;
-    const Shares share(units, p.tile_wgs, kTileLeast);
-    g0 = share.group(at_unit);
-    g1 = share.group(at_unit + units_b - 1);
-    cut = share.first(g0) < at_unit;
+  } else {
+    const int g = (int)blockIdx.x + 1;
+    if (g >= p.tile_cuts[0].x) return;
+    const int4 c = p.tile_cuts[g];
+    row0 = c.x; n_rows = c.y; g0 = g - 1; g1 = c.z; cut = c.w != 0;
   }
+  if ((int)blockIdx.y * per >= n_rows) return;
   const bool complete = g0 == g1;                                 // one workgroup did it all
-  if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
   const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
-  const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + rb * kTileRows + r;
+  const long rows = (long)p.T * p.nH, row = row0 + r;
   RowSum sum;
   if (r < n_rows) {
     sum.add_parts(p.prefix_parts + (complete ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
@@ -464,7 +514,8 @@ template <int D> static hipError_t tile_join_one(const PagedArgs& a, hipStream_t
   int groups = 1;                                                 // one for every 8 parts that a block has on average
   while (groups < 8 && 8 * groups < parts) groups *= 2;
   const int per = SLOTS / groups, most = kTileRows < a.max_new * a.nH ? kTileRows : a.max_new * a.nH;
-  hipLaunchKernelGGL(paged_tile_join_kernel<D>, dim3(blocks, (most + per - 1) / per), dim3(256), 0, s, a, groups);
+  const int first = a.prefix_parts > 0 ? blocks : a.tile_wgs - 1;
+  hipLaunchKernelGGL(paged_tile_join_kernel<D>, dim3(first, (most + per - 1) / per), dim3(256), 0, s, a, groups);
   return hipGetLastError();
 }
 hipError_t launch_paged_tile_join(const PagedArgs& a, hipStream_t s) {
