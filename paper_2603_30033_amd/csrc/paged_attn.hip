@@ -1,10 +1,14 @@
-// Attention over the paged latent cache.
+// Attention over the paged latent cache in fp32, and the join of its partial results.
 //
 // One latent key and value row serves all heads, so the rows of the product are the (token, head) pairs of a sequence, token by
 // token: row r is head r % nH of new token r / nH.  Online softmax over the keys; a row sees the keys up to its token's own.
 //
 //   paged_rows   32 rows a workgroup, its four waves taking every fourth block of 32 keys straight from the pages
 //   paged_merge  joins the partial results of a row: sum_i 2^(m_i - m) (l_i, O_i), m = max m_i
+//
+// The fp32 matrix instructions (64 cycles for 2 channels of 32 x 32) bound many rows; few rows are a chain of dependent loads (where
+// the rows are, page, keys), so the keys of a row block are dealt to two workgroups a compute unit, down to 128 keys, one block a
+// wave, and a block's value loads are on their way beside its key loads.
 #include "paged_block.h"
 
 namespace ta {
@@ -14,8 +18,9 @@ namespace ta {
 // ------------------------------------------------------------------------------------------------------------------
 // Grid: row blocks x parts of the keys.  Key fragments come from memory as they are (a lane reads 16 channels of its key row);
 // value fragments one element a lane, 32 consecutive channels of a row in half a wave.
-template <typename T, int D, bool SH, bool PREFIX>
+template <int D, bool SH, bool PREFIX>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
+  using T = float;
   constexpr int CB = D / 32;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -78,6 +83,19 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
     const int pi = divide(n, p.ps);
     const int page = paged_page(table[min(pi, pages - 1)], p.n_pages), at = n - pi * p.page_size;
     const T* krow = static_cast<const T*>(p.K) + page * p.k_stride + (long)at * p.r3;
+    Frag<T> vf[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int c = min(cb * 32 + lr, p.rt3 - 1);                 // channels behind the last repeat it and are not stored
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = 8 * (e / 4) + 4 * h + e % 4;
+        const long pg = __shfl(page, key), off = __shfl(at, key);
+        const T* src = SH ? static_cast<const T*>(p.K) + pg * p.k_stride + off * p.r3
+                          : static_cast<const T*>(p.V) + pg * p.v_stride + off * p.rt3;
+        frag_set(vf[cb], e, src[c]);
+      }
+    }
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -109,25 +127,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
     for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e] - m_use);
     l_run = block_sum(s, l_run * alpha);
     const Frag<T> pf = to_frag<T>(s);
-    Frag<T> ph;
-    if constexpr (sizeof(T) == 2) ph = rest_of<T>(s, pf);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) oacc[cb][e] *= alpha;
-      Frag<T> vf;
-      const int c = min(cb * 32 + lr, p.rt3 - 1);                 // channels behind the last repeat it and are not stored
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = 8 * (e / 4) + 4 * h + e % 4;
-        const long pg = __shfl(page, key), off = __shfl(at, key);
-        const T* src = SH ? static_cast<const T*>(p.K) + pg * p.k_stride + off * p.r3
-                          : static_cast<const T*>(p.V) + pg * p.v_stride + off * p.rt3;
-        frag_set(vf, e, to_f32(src[c]));
-      }
-      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf)) != 0ull) take_nonfinite<T>(vf, limit - n0 - 4 * h, oacc[cb]);
-      mma32(oacc[cb], vf, pf);
-      if constexpr (sizeof(T) == 2) mma32(oacc[cb], vf, ph);
+      if (__builtin_amdgcn_ballot_w64(!frag_finite(vf[cb])) != 0ull) take_nonfinite<T>(vf[cb], limit - n0 - 4 * h, oacc[cb]);
+      mma32(oacc[cb], vf[cb], pf);
     }
   }
 
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
 // ------------------------------------------------------------------------------------------------------------------
 // partial results of a row joined: a row by D/4 threads, or by `groups` times as many that take every groups-th part
 // ------------------------------------------------------------------------------------------------------------------
-template <typename T, int D>
+template <int D>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p, int groups) {
   constexpr int L = D / 4, SLOTS = 256 / L;
   __shared__ float4 po[256];
@@ -159,7 +164,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p, int group
       o = p.part_o + (i * rows + row) * D + c;
     });
   sum.add_groups(po, pml, slot, group, groups, per, L);
-  if (group == 0 && live) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
+  if (group == 0 && live) paged_result<float>(p, row, c, sum.m, sum.l, sum.o);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -168,42 +173,40 @@ int paged_rows_blocks(const PagedArgs& a, int rows) {
   return (int)(all < 0x7fffffffl ? all : 0x7fffffffl);
 }
 
-template <typename T, int D, bool SH, bool PREFIX> static hipError_t rows_one(const PagedArgs& a, hipStream_t s) {
+template <int D, bool SH, bool PREFIX> static hipError_t rows_one(const PagedArgs& a, hipStream_t s) {
   const size_t smem = join_bytes<D, 1>();
-  auto kern = paged_rows_kernel<T, D, SH, PREFIX>;
+  auto kern = paged_rows_kernel<D, SH, PREFIX>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
   const int blocks = PREFIX ? (int)(((long)a.T * a.nH + 31) / 32) : paged_rows_blocks(a, 32);
   hipLaunchKernelGGL(kern, dim3(blocks, PREFIX ? a.prefix_parts : a.own_parts > 0 ? a.own_parts : 1), dim3(256), smem, s, a);
   return hipGetLastError();
 }
-template <typename T, int D> static hipError_t rows_variant(const PagedArgs& a, bool prefix, hipStream_t s) {
-  if (a.shared_kv) return prefix ? rows_one<T, D, true, true>(a, s) : rows_one<T, D, true, false>(a, s);
-  return prefix ? rows_one<T, D, false, true>(a, s) : rows_one<T, D, false, false>(a, s);
+template <int D> static hipError_t rows_variant(const PagedArgs& a, bool prefix, hipStream_t s) {
+  if (a.shared_kv) return prefix ? rows_one<D, true, true>(a, s) : rows_one<D, true, false>(a, s);
+  return prefix ? rows_one<D, false, true>(a, s) : rows_one<D, false, false>(a, s);
 }
-template <typename T> static hipError_t rows_dispatch(const PagedArgs& a, bool prefix, hipStream_t s) {
+hipError_t launch_paged_rows(const PagedArgs& a, bool prefix, hipStream_t s) {
   switch (a.D) {
-    case 32: return rows_variant<T, 32>(a, prefix, s);
-    case 64: return rows_variant<T, 64>(a, prefix, s);
-    case 128: return rows_variant<T, 128>(a, prefix, s);
+    case 32: return rows_variant<32>(a, prefix, s);
+    case 64: return rows_variant<64>(a, prefix, s);
+    case 128: return rows_variant<128>(a, prefix, s);
   }
   return hipErrorInvalidValue;
 }
-hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s) { return rows_dispatch<float>(a, prefix_pass, s); }
 
-template <typename T> static hipError_t merge_dispatch(const PagedArgs& a, hipStream_t s) {
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s) {
   const long rows = (long)a.T * a.nH;
   int groups = 1;                                                 // 8 parts a thread
   while (groups < 8 && 8 * groups < a.prefix_parts + a.own_parts) groups *= 2;
   auto grid = [&](int slots) { return dim3((uint32_t)((rows + slots / groups - 1) / (slots / groups))); };
   switch (a.D) {
-    case 32: hipLaunchKernelGGL((paged_merge_kernel<T, 32>), grid(32), dim3(256), 0, s, a, groups); break;
-    case 64: hipLaunchKernelGGL((paged_merge_kernel<T, 64>), grid(16), dim3(256), 0, s, a, groups); break;
-    case 128: hipLaunchKernelGGL((paged_merge_kernel<T, 128>), grid(8), dim3(256), 0, s, a, groups); break;
+    case 32: hipLaunchKernelGGL(paged_merge_kernel<32>, grid(32), dim3(256), 0, s, a, groups); break;
+    case 64: hipLaunchKernelGGL(paged_merge_kernel<64>, grid(16), dim3(256), 0, s, a, groups); break;
+    case 128: hipLaunchKernelGGL(paged_merge_kernel<128>, grid(8), dim3(256), 0, s, a, groups); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
-hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s) { return merge_dispatch<float>(a, s); }
 
 }  // namespace ta

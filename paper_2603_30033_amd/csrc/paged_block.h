@@ -19,20 +19,6 @@ template <typename T> __device__ __forceinline__ Frag<T> load_frag_upto(const T*
 }
 
 // the fragment's 8 channel pairs turned by the table entries of their 4 quads
-__device__ __forceinline__ void turn_frag(Frag<bf16>& f, const f32x4 (&cs)[4]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    u32x4 raw = __builtin_bit_cast(u32x4, f.v[i]);
-#pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const float c = cs[2 * i + d / 2][2 * (d % 2)], s = cs[2 * i + d / 2][2 * (d % 2) + 1];
-      const float x0 = __uint_as_float(raw[d] << 16), x1 = __uint_as_float(raw[d] & 0xffff0000u);
-      const f32x2 two = {x0 * c - x1 * s, x0 * s + x1 * c};
-      raw[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2));
-    }
-    f.v[i] = __builtin_bit_cast(bf16x8, raw);
-  }
-}
 __device__ __forceinline__ void turn_frag(Frag<float>& f, const f32x4 (&cs)[4]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q)
@@ -45,8 +31,6 @@ __device__ __forceinline__ void turn_frag(Frag<float>& f, const f32x4 (&cs)[4]) 
 }
 
 __device__ __forceinline__ float frag_at(const Frag<bf16>& f, int e) { return (float)f.v[e / 8][e % 8]; }
-__device__ __forceinline__ float frag_at(const Frag<float>& f, int e) { return f.v[e / 4][e % 4]; }
-__device__ __forceinline__ void frag_set(Frag<bf16>& f, int e, float x) { f.v[e / 8][e % 8] = (bf16)x; }
 __device__ __forceinline__ void frag_set(Frag<float>& f, int e, float x) { f.v[e / 4][e % 4] = x; }
 
 // Values that are not finite where some rows do not see their key: 0 * Inf in a product would reach those rows.  Such values are taken
@@ -123,11 +107,11 @@ template <typename T> __device__ __forceinline__ void take_nonfinite(Frag<T>& v,
 
 // What the rounding of a probability to bf16 left over, as a second operand: without it that rounding (2^-8 at most) would weigh
 // as much in the result as the result's own
-template <typename T> __device__ __forceinline__ Frag<T> rest_of(const f32x16& pr, const Frag<T>& f) {
+__device__ __forceinline__ Frag<bf16> rest_of(const f32x16& pr, const Frag<bf16>& f) {
   f32x16 r;
 #pragma unroll
   for (int e = 0; e < 16; ++e) r[e] = pr[e] - frag_at(f, e);
-  return to_frag<T>(r);
+  return to_frag<bf16>(r);
 }
 
 // lane l's 16 bytes at `from` to chunk l of `to` (the same for the whole wave)

@@ -220,7 +220,7 @@ void paged_stream_kernel(PagedArgs p) {
               x[4 * q + e + 1] = x0 * sn + x1 * c;
             }
           }
-          const Frag<T> kf = to_frag<T>(x), rest = rest_of<T>(x, kf);
+          const Frag<T> kf = to_frag<T>(x), rest = rest_of(x, kf);
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb) {
             mma32(sc[hb], kf, qf[hb][cb]);
@@ -279,7 +279,7 @@ void paged_stream_kernel(PagedArgs p) {
         for (int e = 0; e < 16; ++e) sc[hb][e] = fast_exp2(sc[hb][e] - m_use);
         l_run[hb] = block_sum(sc[hb], l_run[hb]);
         pf[hb] = to_frag<T>(sc[hb]);
-        ph[hb] = rest_of<T>(sc[hb], pf[hb]);
+        ph[hb] = rest_of(sc[hb], pf[hb]);
       }
       if constexpr (kLate) {
 #pragma unroll
