@@ -46,24 +46,24 @@ struct PagedArgs {
   int own_parts;                // then those of the sequence's own rows; 0: written to O directly
   int prefix_keys, own_keys;    // keys of such parts (a short sequence leaves the last parts empty: no output, a sum of 0)
   // The keys of all sequences dealt to this many workgroups (0: a workgroup for every sequence, or row block): of paged_stream, which
-  // takes a sequence's `hb` blocks of 32 rows at once and gives no workgroup less than stream_least units, and of paged_tile.
-  // Rows that several workgroups share leave partial results: [workgroups][hb * 32] rows, [2 * workgroups][kTileRows].
-  int hb, stream_wgs, stream_least, tile_wgs;
-  // paged_tile: work of a key of a row block, 1 / (kTileUnit nH); [0]: number of shares, then for each, if its start is the first in
-  // a row block behind the block's own: first row of the block, its rows (0 otherwise), last share in it, whether the first share
-  // in it begins in an earlier block
-  double tile_per_key;
-  int4* tile_cuts;
+  // takes a sequence's `hb` blocks of 32 rows at once, and of paged_tile.  Rows that several workgroups share leave partial results:
+  // [workgroups][hb * 32] rows, [2 * workgroups][kTileRows].
+  int hb, stream_wgs, tile_wgs;
   float* stream_o;
   float2* stream_ml;
+  int2* stream_parts;           // paged_stream: for every sequence its first workgroup and how many share it
+  double tile_per_key;          // paged_tile: work of a key of a row block, 1 / (kTileUnit nH)
+  // paged_tile: [0]: number of shares, then for each, if its start is the first in a row block behind the block's own: first row of the
+  // block, its rows (0 otherwise), last share in it, whether the first share in it begins in an earlier block
+  int4* tile_cuts;
+  // with a prefix: workgroups of its pieces (a multiple of 8; those above follow in the same launch), and for every row where the
+  // first share left its result and how many shares follow (0: that result is the row's own)
+  int prefix_wgs;
+  int2* tile_rows;
 };
-constexpr int kStreamUnit = 128;       // keys of a unit of that kernel's work
+constexpr int kStreamUnit = 128, kStreamLeast = 2;   // keys of a unit of paged_stream's work, least units of a workgroup
 // whether two of its workgroups share a compute unit by design (KIND 1: one pool, keys rotated on use)
 constexpr bool stream_late(int D, int kind) { return D == 128 && kind == 1; }
-// workgroups that share B sequences where `wgs` are wanted: with few sequences no more than that, else every sequence's last part
-// may be one more
-inline int stream_grid(int B, int wgs) { return 2l * B <= wgs ? wgs : wgs + B; }
-
 // Latent rows into their pages, keys (and the per-head queries, if given) rotated to the tokens' positions
 struct PagedAppendArgs {
   void *K, *V;                  // pools as above

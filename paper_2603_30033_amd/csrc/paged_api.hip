@@ -1,4 +1,6 @@
 // Host side of the paged latent cache: argument checks, the split of a call's work, launches.
+#include <algorithm>
+
 #include "context.h"
 #include "paged.h"
 
@@ -65,24 +67,31 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   a.B = b->B; a.T = b->T; a.nH = f.n_heads; a.D = c->D; a.prefix = prefix;
   const long rows = (long)b->T * f.n_heads, most = (long)b->max_new * f.n_heads;
   const int keys = b->max_len - prefix;
-  a.hb = f.dtype != TUCKER_ATTN_BF16 ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
-  const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // paged_tile: fp32 rows go through paged_rows
+  const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // (fp32 rows go through paged_rows)
   const int block = tile ? kTileRows : 32;
   a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, tile ? 1 : 2, tile ? 256 : 128) : 0;
   a.prefix_keys = a.prefix_parts > 0 ? part_keys(prefix, a.prefix_parts) : 0;
+  const long pieces = (rows + block - 1) / block * a.prefix_parts;
+  a.prefix_wgs = (int)((pieces + 7) / 8 * 8);
+  // Few rows and no prefix: paged_stream, unless there are so many sequences that its workgroups could not have equal shares.  us,
+  // 32 heads of 128 channels, paged_stream and paged_tile: 128 sequences of up to 1024 rows 22, 24; 140: 32, 25; 200: 37, 27; 16 of 4096
+  // 21, 22; one of 32768 19, 21; 12 heads of 64: 1 of 257 8, 12; 140 of 3000 28, 24; a shared latent: 140 of 3000 37, 42, 250 68, 55.
+  // Behind a prefix their keys go with the prefix's own launch, which paged_tile does (two launches of these kernels: 32 sequences
+  // behind 16384 rows 44 and 35; 128 with up to 1024 rows of their own 46 and 33; 16 with 32768 68 and 57).
+  const int wgs = (stream_late(c->D, f.shared_kv && f.use_rope ? 1 : 0) ? 2 : 1) * c->n_cus;
+  const bool split = keys > kStreamWhole;
+  a.hb = !tile || prefix > 0 || (split && (2 * (long)b->B > wgs || b->B > 256)) ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
   a.stream_wgs = a.tile_wgs = 0;
   a.own_parts = prefix > 0 ? 1 : 0;                               // rows that one workgroup does alone
   long shared = 0;                                                // rows of partial results that workgroups share
   if (a.hb > 0) {
-    // (with a prefix a second launch joins the results anyway)
-    a.stream_least = prefix > 0 ? 1 : 2;
-    if (keys > (prefix > 0 ? kStreamUnit : kStreamWhole)) {
-      a.stream_wgs = (stream_late(c->D, f.shared_kv && f.use_rope ? 1 : 0) ? 2 : 1) * c->n_cus;
-      shared = (long)stream_grid(b->B, a.stream_wgs) * a.hb * 32;
+    if (split) {
+      a.stream_wgs = wgs;
+      shared = (long)wgs * a.hb * 32;
     }
   } else if (tile) {
     const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
-    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31)) a.tile_wgs = 2 * c->n_cus;
+    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31)) a.tile_wgs = std::max(2 * c->n_cus - (int)std::min(pieces, 2l * c->n_cus), c->n_cus);
     a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
@@ -96,7 +105,9 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   a.part_ml = cv.take<float2>(parts * rows * 8);
   a.stream_o = cv.take<float>(shared * c->D * 4);
   a.stream_ml = cv.take<float2>(shared * 8);
-  a.tile_cuts = cv.take<int4>(a.tile_wgs * sizeof(int4));
+  a.stream_parts = cv.take<int2>(a.stream_wgs > 0 ? b->B * sizeof(int2) : 0);
+  a.tile_cuts = cv.take<int4>(prefix > 0 ? 0 : a.tile_wgs * sizeof(int4));
+  a.tile_rows = cv.take<int2>(tile && prefix > 0 ? rows * sizeof(int2) : 0);
   return cv.off;
 }
 
@@ -121,9 +132,11 @@ int launch_attend(const tucker_attn_ctx* c, const PagedArgs& a, hipStream_t s, R
     if ((tile ? launch_paged_tile(a, true, s) : launch_paged_rows(a, true, s)) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
     (void)rec.after("prefix_attention");
   }
-  if ((a.hb > 0 ? launch_paged_stream(a, s) : tile ? launch_paged_tile(a, false, s) : launch_paged_rows(a, false, s)) != hipSuccess)
-    return TUCKER_ATTN_HIP_ERROR;
-  (void)rec.after("paged_attention");
+  if (a.prefix == 0 || !tile) {                                   // (that launch of paged_tile did the sequences' own keys as well)
+    if ((a.hb > 0 ? launch_paged_stream(a, s) : tile ? launch_paged_tile(a, false, s) : launch_paged_rows(a, false, s)) != hipSuccess)
+      return TUCKER_ATTN_HIP_ERROR;
+    (void)rec.after("paged_attention");
+  }
   if (a.prefix_parts + a.own_parts + a.stream_wgs + a.tile_wgs > 0) {
     if ((a.hb > 0 ? launch_paged_join(a, s) : tile ? launch_paged_tile_join(a, s) : launch_paged_merge(a, s)) != hipSuccess)
       return TUCKER_ATTN_HIP_ERROR;

@@ -6,6 +6,7 @@
 //   - The key rows of a sequence are cut into units of 128 and dealt to workgroups, the same number to each whatever the
 //     sequence: as many as give every compute unit one workgroup.  (A workgroup finds its part by a scan over the lengths, which
 //     live on the device.)  Where several share a sequence each leaves (max, sum, output) of its rows, which paged_join adds up.
+//     More sequences than half the workgroups would leave parts of very different lengths: those go through paged_tile.
 //   - Wave w takes keys 32w .. 32w+31 of a unit and does all the work for them (scores of every row, its own running softmax,
 //     product with the values): nothing is shared between the waves while they stream, so there is no barrier in the loop.
 //   - Rows go from the pages straight into the wave's two LDS stages, two units ahead.
@@ -28,7 +29,7 @@ template <int D, int KIND> struct StreamLds {
 // units of sequence b (no new token: none; no key of its own: one, which leaves its rows' empty result)
 __device__ __forceinline__ int stream_units(const PagedArgs& p, int b) {
   const PagedSeq s = paged_seq(p, b);
-  return (int)(s.nq != 0) * max(1, (s.len - p.prefix + kUnit - 1) / kUnit);   // (no branch: the loads go together)
+  return (int)(s.nq != 0) * max(1, (s.len + kUnit - 1) / kUnit);  // (no branch: the loads go together)
 }
 // sum of every thread's number; all 256 threads call, sh holds 4 words
 __device__ __forceinline__ int block_total(int x, int* sh) {
@@ -39,32 +40,14 @@ __device__ __forceinline__ int block_total(int x, int* sh) {
   __syncthreads();
   return sh[0] + sh[1] + sh[2] + sh[3];
 }
-// Units of a workgroup.  One round of workgroups over the compute units if that can be had: the units' share of each, or, where the
-// sequences' last parts make too many of these, a share that is larger by as much.
-struct StreamShare {
-  const PagedArgs& p;
-  int mine;                                                       // units of sequence threadIdx.x
-  int units;                                                      // of a workgroup
-  __device__ __forceinline__ StreamShare(const PagedArgs& a, int* sh) : p(a) {
-    mine = (int)threadIdx.x < p.B ? stream_units(p, threadIdx.x) : 0;
-    auto total = [&](auto f) {
-      int n = (int)threadIdx.x < p.B ? f(mine) : 0;
-      for (int i = threadIdx.x + 256; i < p.B; i += 256) n += f(stream_units(p, i));
-      return block_total(n, sh);
-    };
-    const int all = total([](int n) { return n; });
-    units = max(p.stream_least, (all + p.stream_wgs - 1) / p.stream_wgs);
-    if (2 * p.B <= p.stream_wgs) {
-      const int t = units;
-      if (total([=](int n) { return (n + t - 1) / t; }) > p.stream_wgs)
-        units = max(units, (all + p.stream_wgs - p.B - 1) / (p.stream_wgs - p.B));
-    }
-  }
-  __device__ __forceinline__ int parts(int b) const {             // workgroups of sequence b
-    const int n = b == (int)threadIdx.x ? mine : stream_units(p, b);
-    return (n + units - 1) / units;
-  }
-};
+// Units of a workgroup where `mine` are thread i's sequence's (at most 256 sequences, and no more than half the workgroups): one round
+// of workgroups over the compute units, the units' share of each, or, where the sequences' last parts make too many of these, a share
+// that is larger by as much.
+__device__ __forceinline__ int stream_share(const PagedArgs& p, int mine, int* sh) {
+  const int all = block_total(mine, sh), units = max(kStreamLeast, (all + p.stream_wgs - 1) / p.stream_wgs);
+  if (block_total((mine + units - 1) / units, sh) <= p.stream_wgs) return units;
+  return max(units, (all + p.stream_wgs - p.B - 1) / (p.stream_wgs - p.B));
+}
 
 template <int D, int HB, int KIND>
 // Wide latents with two pools: LDS leaves one wave to a SIMD, which may then use all registers.  With one pool whose keys are rotated on
@@ -86,14 +69,16 @@ void paged_stream_kernel(PagedArgs p) {
     cnt = stream_units(p, b);
   } else {
     int* sh = reinterpret_cast<int*>(smem_raw);
-    const StreamShare share(p, sh);
+    const int mine = (int)threadIdx.x < p.B ? stream_units(p, threadIdx.x) : 0, units = stream_share(p, mine, sh);
     int part, all;
     __syncthreads();
-    b = paged_locate(p.B, blockIdx.x, [&](int i) { return share.parts(i); }, sh, part, all);
+    b = paged_locate(p.B, blockIdx.x, [&](int) { return (mine + units - 1) / units; }, sh, part, all);   // (a sequence for every thread)
     if (b < 0) return;
     b = __builtin_amdgcn_readfirstlane(b);
-    off = __builtin_amdgcn_readfirstlane(part) * share.units;
-    cnt = min(share.units, stream_units(p, b) - off);
+    off = __builtin_amdgcn_readfirstlane(part) * units;
+    const int n = stream_units(p, b);
+    cnt = min(units, n - off);
+    if (off == 0 && threadIdx.x == 0) p.stream_parts[b] = int2{(int)blockIdx.x, (n + units - 1) / units};   // for the join
   }
   if (cnt == 0) return;
 
@@ -102,7 +87,7 @@ void paged_stream_kernel(PagedArgs p) {
   const PagedSeq s = paged_seq(p, b);
   const int all = stream_units(p, b);
   const int keys = s.len, n_rows = s.nq * p.nH, row0 = s.q0 * p.nH;
-  const int unit0 = p.prefix + off * kUnit;                     // first key
+  const int unit0 = off * kUnit;                                // first key
   const int* table = p.table + (long)b * p.max_pages;
   const int lo = p.causal ? keys - s.nq + 1 : keys;             // keys that every row sees
 
@@ -125,7 +110,7 @@ void paged_stream_kernel(PagedArgs p) {
     // their row and chunk to it.  Rows behind the sequence's last are whatever the page holds, chunks behind a row's end (which meet
     // zeros of the queries, or become channels that are not stored) repeat its last.  Else every lane looks up its own rows.
     constexpr int PPG = 16 / RPP;                                 // pieces of 16 rows
-    const bool straight = p.page_size % 16 == 0 && p.prefix % 16 == 0;
+    const bool straight = p.page_size % 16 == 0;
     auto block_at = [&](int j) { return unit0 + min(j, cnt - 1) * kUnit + wave * 32; };   // past the end: the last again, unused
     const auto* entries = (const __attribute__((address_space(4))) int*)table;
     auto entry_at = [&](int j, int half) {
@@ -325,59 +310,39 @@ void paged_stream_kernel(PagedArgs p) {
   }
   __syncthreads();
 
-  const bool complete = off == 0 && cnt == all, direct = complete && p.prefix_parts == 0;
-  const long slot0 = complete ? (long)p.prefix_parts * p.T * p.nH + row0 : (long)blockIdx.x * (HB * 32);
-  float* po = complete ? p.part_o : p.stream_o;
-  float2* pml = complete ? p.part_ml : p.stream_ml;
+  const bool complete = off == 0 && cnt == all;
   join_waves<D, HB>(reinterpret_cast<float*>(smem_raw), oacc, m_run, l_run, n_rows, [&](int row, int c, float m, float l, f32x4 o) {
-    if (direct) paged_result<T>(p, (long)row0 + row, c, m, l, o);
-    else paged_partial<D>(po, pml, slot0 + row, c, m, l, o);
+    if (complete) paged_result<T>(p, (long)row0 + row, c, m, l, o);
+    else paged_partial<D>(p.stream_o, p.stream_ml, (long)blockIdx.x * (HB * 32) + row, c, m, l, o);
   });
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// The partial results of a sequence's rows: those of the prefix, and its own.  Grid: sequences x groups of rows; a row by D/4
-// threads, as many rows a workgroup as leave every part of a row a group of threads of its own (up to 8 groups).
+// The partial results of a sequence's rows, from the workgroups that the first of them has named.  Grid: sequences x groups of rows; a
+// row by D/4 threads, as many rows a workgroup as leave every part of a row a group of threads of its own (up to 8 groups).
 // ------------------------------------------------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups) {
   using T = bf16;
   constexpr int L = D / 4, SLOTS = 256 / L;                       // threads of a row, rows or groups of a workgroup
-  __shared__ int sums[8];
   __shared__ float4 po[256];
   __shared__ float2 pml[SLOTS];
   const int b = blockIdx.x, tid = threadIdx.x;
   const PagedSeq s = paged_seq(p, b);
   const int n_rows = s.nq * p.nH, per = SLOTS / groups;
   if ((int)blockIdx.y * per >= n_rows) return;
-
-  int g0 = 0, own = 1;                                            // first of the workgroups that share the sequence, their number
-  if (p.stream_wgs > 0) {
-    const StreamShare share(p, sums);
-    int before = 0;
-    for (int i = tid; i < b; i += 256) before += share.parts(i);
-    g0 = block_total(before, sums);
-    own = (stream_units(p, b) + share.units - 1) / share.units;
-  }
-  const bool complete = own == 1;                                 // one workgroup did it all
-  if (complete && p.prefix_parts == 0) return;                    // ... and has written the result
+  const int2 parts = p.stream_parts[b];
+  if (parts.y == 1) return;                                       // one workgroup did it all and has written the result
   const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
-  const long rows = (long)p.T * p.nH, row = (long)s.q0 * p.nH + r;
   RowSum sum;
-  if (r < n_rows) {
-    sum.add_parts(p.prefix_parts + (complete ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
-      ml = p.part_ml + i * rows + row;
-      o = p.part_o + (i * rows + row) * D + c;
+  if (r < n_rows)
+    sum.add_parts(parts.y, group, groups, [&](int i, const float2*& ml, const float*& o) {
+      const long at = (long)(parts.x + i) * (p.hb * 32) + r;
+      ml = p.stream_ml + at;
+      o = p.stream_o + at * D + c;
     });
-    if (!complete)
-      sum.add_parts(own, group, groups, [&](int i, const float2*& ml, const float*& o) {
-        const long at = (long)(g0 + i) * (p.hb * 32) + r;
-        ml = p.stream_ml + at;
-        o = p.stream_o + at * D + c;
-      });
-  }
   sum.add_groups(po, pml, slot, group, groups, per, L);
-  if (group == 0 && r < n_rows) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
+  if (group == 0 && r < n_rows) paged_result<T>(p, (long)s.q0 * p.nH + r, c, sum.m, sum.l, sum.o);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -386,7 +351,7 @@ template <int D, int HB, int KIND> static hipError_t stream_one(const PagedArgs&
   auto kern = paged_stream_kernel<D, HB, KIND>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3(a.stream_wgs > 0 ? stream_grid(a.B, a.stream_wgs) : a.B), dim3(256), smem, s, a);
+  hipLaunchKernelGGL(kern, dim3(a.stream_wgs > 0 ? a.stream_wgs : a.B), dim3(256), smem, s, a);
   return hipGetLastError();
 }
 template <int D> static hipError_t stream_variant(const PagedArgs& a, hipStream_t s) {
@@ -407,7 +372,7 @@ hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s) {
 template <int D> static hipError_t join_one(const PagedArgs& a, hipStream_t s) {
   constexpr int SLOTS = 256 / (D / 4);
   // one group of threads for every 8 parts that a sequence has on average
-  const int parts = a.prefix_parts + (a.stream_wgs > 0 ? a.stream_wgs / a.B : 0) + 1;
+  const int parts = a.stream_wgs / a.B + 1;
   int groups = 1;
   while (groups < 8 && 8 * groups < parts) groups *= 2;
   const int per = SLOTS / groups, most = a.max_new * a.nH;

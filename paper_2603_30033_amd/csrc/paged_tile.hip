@@ -61,10 +61,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // ---- which rows, which keys ----
   // Workgroups go to the eight dies in turn, and each die has a cache of its own: workgroup i of a die takes piece i of the die's
   // share of consecutive pieces, which read the same keys.
-  const int die = blockIdx.x % 8, in_die = blockIdx.x / 8;
+  const bool pre = PREFIX && (int)blockIdx.x < p.prefix_wgs;      // the prefix's pieces come first, then shares of the sequences' own keys
+  const int wg = PREFIX && !pre ? blockIdx.x - p.prefix_wgs : blockIdx.x;
+  const int die = wg % 8, in_die = wg / 8;
   // sequence, row block, items of its work that others do before, all its items, items to do
   int b = 0, rb, item = 0, items = 1, left = 1, part = 0, me = 0;
-  if constexpr (PREFIX) {
+  Shares shares(0, 1, 1);
+  int done = 0;                                                   // items in front of this share and of the segments behind
+  if (pre) {
     const int blocks = (p.T * p.nH + RB - 1) / RB, per = (blocks * p.prefix_parts + 7) / 8, piece = die * per + in_die;
     if (in_die >= per || piece >= blocks * p.prefix_parts) return;
     part = piece / blocks;
@@ -72,30 +76,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   } else {
     int index, all;
     if (p.tile_wgs == 0) {                                        // a workgroup for every row block
-      b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
+      b = paged_locate(p.B, wg, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
       if (b < 0) return;
     } else {
       auto work = [&](int i) { return tile_work(p, i); };
       b = paged_locate(p.B, 0, work, reinterpret_cast<int*>(smem_raw), index, all);
       if (b < 0) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) p.tile_cuts[0].x = 0;
+        if (!PREFIX && blockIdx.x == 0 && threadIdx.x == 0) p.tile_cuts[0].x = 0;
         return;
       }
       const Shares sh(all, p.tile_wgs, kTileLeast);
       const int per = (sh.G + 7) / 8;
       me = die * per + in_die;
       if (in_die >= per || me >= sh.G) return;
-      const int mine = sh.first(me);
-      left = sh.first(me + 1) - mine;
-      if (me > 0) b = paged_locate(p.B, mine, work, reinterpret_cast<int*>(smem_raw), index, all);
+      done = sh.first(me);
+      shares = sh;
+      left = sh.first(me + 1) - done;
+      if (me > 0) b = paged_locate(p.B, done, work, reinterpret_cast<int*>(smem_raw), index, all);
       b = __builtin_amdgcn_readfirstlane(b);
       index = __builtin_amdgcn_readfirstlane(index);
       const PagedSeq s = paged_seq(p, b);
       rb = tile_block(p, s, index);
       item = index - tile_work(p, s, rb);
       items = tile_work(p, s, rb + 1) - tile_work(p, s, rb);
-      if (threadIdx.x == 0) {                                     // for the join: how many shares there are, what starts in a block
-        const int at = mine - item;
+      if (!PREFIX && threadIdx.x == 0) {                          // for the join: how many shares there are, what starts in a block
+        const int at = done - item;
         if (me == 0) p.tile_cuts[0].x = sh.G;
         else if (item == 0 || sh.group(at) != me - 1) p.tile_cuts[me].y = 0;   // at its start; behind another share's start
         else
@@ -110,7 +115,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   for (int segment = 0; left > 0; ++segment) {
   int row0 = 0, first = 0, nq, len = p.prefix, pages;             // first row of the sequence in [T * nH], its first key, ..
   const int* table = p.prefix_table;
-  if constexpr (PREFIX) {
+  if (pre) {
     nq = min(max(p.q_start[p.B], 0), p.T);
     pages = divide(p.prefix - 1, p.ps) + 1;
     if (rb * RB >= nq * p.nH) return;
@@ -123,8 +128,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     table = p.table + (long)b * p.max_pages;
     pages = p.max_pages;
   }
-  const int n_rows = nq * p.nH, now = PREFIX ? 1 : min(left, items - item);
-  const bool causal = !PREFIX && p.causal;
+  const int n_rows = nq * p.nH, now = pre ? 1 : min(left, items - item);
+  const bool causal = !pre && p.causal;
   const int r0 = rb * RB, rw = r0 + wave * 32;                 // first row of the workgroup, of this wave
   const int r = min(rw + lr, n_rows - 1);                         // rows behind the last repeat it and are not stored
   auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
@@ -133,9 +138,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // items dealt to whole units of the keys that the block sees; who ends here and who goes on from here count alike
   const int units = max(0, hi_all - first + kTileUnit - 1) / kTileUnit;
   auto unit_at = [&](int i) { return i == 0 ? 0 : i == items ? units : __builtin_amdgcn_readfirstlane((int)((double)i * units / items)); };
-  const int key0 = PREFIX ? part * p.prefix_keys : first + unit_at(item) * kTileUnit;
-  const int key1 = min(hi_all, PREFIX ? key0 + p.prefix_keys : first + unit_at(item + now) * kTileUnit);
+  const int key0 = pre ? part * p.prefix_keys : first + unit_at(item) * kTileUnit;
+  const int key1 = min(hi_all, pre ? key0 + p.prefix_keys : first + unit_at(item + now) * kTileUnit);
   const int cnt = key1 > key0 ? (key1 - key0 + BC - 1) / BC : 0;  // tiles
+  const bool busy = rw < n_rows;                                  // a wave without rows helps with the loads only
 
   f32x16 oacc[CB];
   float m_run = -INFINITY, l_run = 0.f;
@@ -305,12 +311,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       for (; j < n_whole; ++j) {
         arrived();
         fill(j + 1, (j + 1) & 1);                                 // into the stage of tile j - 1
-        whole(j & 1);
+        if (busy) whole(j & 1);
       }
       for (; j < cnt; ++j) {
         arrived();
         fill(j + 1, (j + 1) & 1);
-        edge(j, j & 1);
+        if (busy) edge(j, j & 1);
       }
       wait_vm<0>();                                               // tiles requested past the end still land in LDS
     } else {
@@ -364,27 +370,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         __syncthreads();
         store((j + 1) & 1);                                       // the stage of tile j - 1
         load(j + 2);
-        whole(j & 1);
+        if (busy) whole(j & 1);
       }
       for (; j < cnt; ++j) {                                      // (nothing is kept in registers for later: they are all in use)
         __syncthreads();
         load(j + 1);
         store((j + 1) & 1);
-        edge(j, j & 1);
+        if (busy) edge(j, j & 1);
       }
     }
   }
 
   // ---- the rows: a result, or a part of one ----
   const float l = halves_sum(l_run);
-  const bool complete = !PREFIX && now == items;                  // nobody else has keys of these rows
+  const bool complete = !pre && now == items;                     // nobody else has keys of these rows
   if (rw + lr < n_rows) {
     const long at = (long)row0 + rw + lr;
-    const bool direct = complete && p.prefix_parts == 0;
-    const bool by_row = PREFIX || complete;
-    const long slot = by_row ? (long)(PREFIX ? part : p.prefix_parts) * p.T * p.nH + at : (2l * me + (segment > 0)) * RB + wave * 32 + lr;
+    const bool direct = complete && !PREFIX;
+    const bool by_row = pre || complete;
+    const int shared = (2 * me + (segment > 0)) * RB + wave * 32 + lr;
+    const long slot = by_row ? (long)(pre ? part : p.prefix_parts) * p.T * p.nH + at : shared;
     float* po = by_row ? p.part_o : p.stream_o;
     float2* pml = by_row ? p.part_ml : p.stream_ml;
+    // for the join: this share, the first of the row's, and how many more there are
+    if (PREFIX && !pre && item == 0 && h == 0)
+      p.tile_rows[at] = int2{shared, complete ? 0 : shares.group(done + items - 1) - me};
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -396,7 +406,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       }
   }
   left -= now;
-  if (PREFIX || left == 0) break;
+  done += now;
+  if (pre || left == 0) break;
   item = 0;
   PagedSeq s = paged_seq(p, b);
   if (++rb == tile_blocks(p, s)) {
@@ -410,78 +421,57 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// The partial results of a row block: those of the prefix, and its own.  Grid: row blocks x groups of rows; without a prefix only
-// blocks that are shared have something to join, so the grid has the shares in place of the row blocks, and the workgroup that did
-// a share has left what there is to join at its start (to look for it here again: 20 us more).  A row by D/4 threads, or by `groups`
-// times as many.
+// The partial results of rows that several workgroups share, or that have a prefix.  A row by D/4 threads, or by `groups` times as
+// many.  Without a prefix only the row blocks in which a share starts have something to join (grid: shares x groups of rows), with one
+// all rows have.  What there is to join for a block or row the workgroup that did its first share has left in memory (to look for it
+// here again: 20 us more).
 // ------------------------------------------------------------------------------------------------------------------
-template <int D>
+template <int D, bool PREFIX>
 __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int groups) {
   using T = bf16;
   constexpr int L = D / 4, SLOTS = 256 / L;
-  __shared__ int sh[8];
   __shared__ float4 po[256];
   __shared__ float2 pml[SLOTS];
-  const int tid = threadIdx.x, per = SLOTS / groups;
-  int n_rows, g0 = 0, g1 = 0;                                     // workgroups that share the block,
-  bool cut = false;                                               // the first of them behind another block
-  long row0;
-  if (p.prefix_parts > 0) {
-    int rb, all;
-    const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, sh, rb, all);
-    if (b < 0) return;
-    const PagedSeq s = paged_seq(p, b);
-    row0 = (long)s.q0 * p.nH + rb * kTileRows;
-    n_rows = min(s.nq * p.nH - rb * kTileRows, kTileRows);
-    if (p.tile_wgs > 0) {
-      int before = 0;
-      all = 0;
-      for (int i = tid; i < p.B; i += 256) {
-        const int n = tile_work(p, i);
-        all += n;
-        if (i < b) before += n;
-      }
-#pragma unroll
-      for (int d = 1; d < kWave; d *= 2) {
-        all += __shfl_xor(all, d);
-        before += __shfl_xor(before, d);
-      }
-      if (tid % kWave == 0) {
-        sh[tid / kWave] = all;
-        sh[4 + tid / kWave] = before;
-      }
-      __syncthreads();
-      const int first = tile_work(p, s, rb), at = sh[4] + sh[5] + sh[6] + sh[7] + first;
-      const Shares share(sh[0] + sh[1] + sh[2] + sh[3], p.tile_wgs, kTileLeast);
-      g0 = share.group(at);
-      g1 = share.group(at + tile_work(p, s, rb + 1) - first - 1);
-      cut = share.first(g0) < at;
-    }
+  const int tid = threadIdx.x, per = SLOTS / groups, slot = tid / L, c = tid % L * 4, group = slot / per;
+  const long rows = (long)p.T * p.nH;
+  long row;
+  int first, more;                                                // slot of the first share's result; shares behind it
+  bool live;
+  if constexpr (PREFIX) {
+    row = (long)blockIdx.x * per + slot % per;
+    const int q0 = min(max(p.q_start[0], 0), p.T), q1 = min(max(p.q_start[p.B], 0), p.T);
+    live = row >= (long)q0 * p.nH && row < (long)q1 * p.nH;       // not behind the last sequence
+    const int2 e = live ? p.tile_rows[row] : int2{0, 0};
+    // (bounded: a row that no sequence has, where q_start says less than it should, finds anything here)
+    first = min(max(e.x, 0), max(2 * p.tile_wgs * kTileRows - 1, 0));
+    more = min(max(e.y, 0), max(p.tile_wgs - 1 - first / (2 * kTileRows), 0));
   } else {
-    const int g = (int)blockIdx.x + 1;
+    const int g = (int)blockIdx.x + 1, r = (int)blockIdx.y * per + slot % per;
     if (g >= p.tile_cuts[0].x) return;
-    const int4 c = p.tile_cuts[g];
-    row0 = c.x; n_rows = c.y; g0 = g - 1; g1 = c.z; cut = c.w != 0;
+    const int4 e = p.tile_cuts[g];
+    if ((int)blockIdx.y * per >= e.y) return;
+    live = r < e.y;
+    row = (long)e.x + r;
+    first = (2 * (g - 1) + e.w) * kTileRows + r;
+    more = e.z - (g - 1);
   }
-  if ((int)blockIdx.y * per >= n_rows) return;
-  const bool complete = g0 == g1;                                 // one workgroup did it all
-  const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
-  const long rows = (long)p.T * p.nH, row = row0 + r;
   RowSum sum;
-  if (r < n_rows) {
-    sum.add_parts(p.prefix_parts + (complete ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
-      ml = p.part_ml + i * rows + row;
-      o = p.part_o + (i * rows + row) * D + c;
-    });
-    if (!complete)
-      sum.add_parts(g1 - g0 + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
-        const long at = (2l * (g0 + i) + (cut && i == 0)) * kTileRows + r;
+  if (live) {
+    if (PREFIX)
+      sum.add_parts(p.prefix_parts + (more == 0 ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
+        ml = p.part_ml + i * rows + row;
+        o = p.part_o + (i * rows + row) * D + c;
+      });
+    if (more > 0)
+      sum.add_parts(more + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
+        // share i's first segment, but the first share's last
+        const long at = i == 0 ? first : (first / (2 * kTileRows) + i) * 2l * kTileRows + first % kTileRows;
         ml = p.stream_ml + at;
         o = p.stream_o + at * D + c;
       });
   }
   sum.add_groups(po, pml, slot, group, groups, per, L);
-  if (group == 0 && r < n_rows) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
+  if (group == 0 && live) paged_result<T>(p, row, c, sum.m, sum.l, sum.o);
 }
 
 template <int D, int KIND, bool PREFIX> static hipError_t tile_one(const PagedArgs& a, hipStream_t s) {
@@ -489,8 +479,7 @@ template <int D, int KIND, bool PREFIX> static hipError_t tile_one(const PagedAr
   auto kern = paged_tile_kernel<D, KIND, PREFIX>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
-  const long blocks = PREFIX ? ((long)a.T * a.nH + kTileRows - 1) / kTileRows * a.prefix_parts : a.tile_wgs;
-  const uint32_t grid = !PREFIX && a.tile_wgs == 0 ? paged_rows_blocks(a, kTileRows) : (uint32_t)((blocks + 7) / 8 * 8);
+  const uint32_t own = a.tile_wgs == 0 ? paged_rows_blocks(a, kTileRows) : (uint32_t)((a.tile_wgs + 7) / 8 * 8), grid = own + (PREFIX ? a.prefix_wgs : 0);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), smem, s, a);
   return hipGetLastError();
 }
@@ -511,11 +500,13 @@ hipError_t launch_paged_tile(const PagedArgs& a, bool prefix_pass, hipStream_t s
 template <int D> static hipError_t tile_join_one(const PagedArgs& a, hipStream_t s) {
   constexpr int SLOTS = 256 / (D / 4);
   const int blocks = paged_rows_blocks(a, kTileRows), parts = a.prefix_parts + (a.tile_wgs > 0 ? a.tile_wgs / blocks : 0) + 1;
-  int groups = 1;                                                 // one for every 8 parts that a block has on average
+  int groups = 1;                                                 // one for every 8 parts that a row has on average
   while (groups < 8 && 8 * groups < parts) groups *= 2;
   const int per = SLOTS / groups, most = kTileRows < a.max_new * a.nH ? kTileRows : a.max_new * a.nH;
-  const int first = a.prefix_parts > 0 ? blocks : a.tile_wgs - 1;
-  hipLaunchKernelGGL(paged_tile_join_kernel<D>, dim3(first, (most + per - 1) / per), dim3(256), 0, s, a, groups);
+  if (a.prefix_parts > 0)
+    hipLaunchKernelGGL((paged_tile_join_kernel<D, true>), dim3(((long)a.T * a.nH + per - 1) / per), dim3(256), 0, s, a, groups);
+  else
+    hipLaunchKernelGGL((paged_tile_join_kernel<D, false>), dim3(a.tile_wgs - 1, (most + per - 1) / per), dim3(256), 0, s, a, groups);
   return hipGetLastError();
 }
 hipError_t launch_paged_tile_join(const PagedArgs& a, hipStream_t s) {
