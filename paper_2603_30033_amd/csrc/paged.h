@@ -43,7 +43,7 @@ struct PagedArgs {
   float* part_o;                // [parts][T * nH][D]
   float2* part_ml;              // [parts][T * nH]
   int prefix_parts;             // parts 0 .. prefix_parts-1: the prefix
-  int own_parts;                // then those of the sequence's own rows; 0: written to O directly
+  int own_parts;                // then those of the sequence's own rows (bf16: one, of rows that one workgroup does alone); 0: written to O
   int prefix_keys, own_keys;    // keys of such parts (a short sequence leaves the last parts empty: no output, a sum of 0)
   // The keys of all sequences dealt to this many workgroups (0: a workgroup for every sequence, or row block): of paged_stream, which
   // takes a sequence's `hb` blocks of 32 rows at once, and of paged_tile.  Rows that several workgroups share leave partial results:

@@ -6,13 +6,18 @@
 // bound for many tokens, and for few a chain of four dependent reads (batch bounds, length, table entry, rotation).
 //
 // A group of CH = r3/8 (bf16) lanes takes one token's rows by 16-byte chunks, a lane the same channels of every row: it reads its
-// rotation once and applies it to up to kHeads query rows, whose loads are all in flight before the first is used.
+// rotation once and applies it to up to kAppendHeads query rows, whose loads are all in flight before the token's sequence is looked
+// for (8189 tokens of 32 heads of 128 channels: 37.1 us, looked for first 38.5; with 4, 16 heads a group 38.6, 45.0).  Rotated queries
+// that no L2 can hold until they are read go past the caches, which leaves these to what the call still has to read: the same call
+// 26 us (5.5 TB/s; a large copy has 4.9), together with the attention behind it 407 us for two prompts of 4096 tokens and 404
+// without.  Queries in place are in the caches already.  One token of 12 heads of 64 channels: 5.0 us, of which the launch is half.
 #include "paged.h"
 
 namespace ta {
 
 constexpr int kAppendHeads = 8;         // query rows of a group
 constexpr int kAppendStarts = 1024;     // batch bounds looked through at a time
+constexpr long kL2Bytes = 32l << 20;    // of all eight dies
 
 template <typename T> struct Row16 {    // 16 bytes of a row as fp32
   static constexpr int N = 16 / (int)sizeof(T);
@@ -35,7 +40,7 @@ template <typename T, bool WIDE> __device__ __forceinline__ void load16(const T*
     for (int i = 0; i < Row16<T>::N; ++i) r.x[i] = to_f32(p[i]);
   }
 }
-template <typename T, bool WIDE> __device__ __forceinline__ void store16(T* p, const Row16<T>& r) {
+template <typename T, bool WIDE, bool PAST = false> __device__ __forceinline__ void store16(T* p, const Row16<T>& r) {
   if constexpr (WIDE) {
     u32x4 raw;
 #pragma unroll
@@ -47,7 +52,8 @@ template <typename T, bool WIDE> __device__ __forceinline__ void store16(T* p, c
         raw[i] = __float_as_uint(r.x[i]);
       }
     }
-    *reinterpret_cast<u32x4*>(p) = raw;
+    if constexpr (PAST) __builtin_nontemporal_store(raw, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = raw;
   } else {
 #pragma unroll
     for (int i = 0; i < Row16<T>::N; ++i) store1(p + i, r.x[i]);
@@ -62,8 +68,8 @@ template <typename T> __device__ __forceinline__ void turn(Row16<T>& r, const f3
   }
 }
 
-// WIDE: every row starts on 16 bytes.  parts: groups that a token's rows are dealt to, the last of them its key and value row
-template <typename T, bool WIDE>
+// WIDE: every row starts on 16 bytes.  PAST: rotated queries go past the caches.  parts: groups that a token's rows are dealt to, the last of them its key and value row
+template <typename T, bool WIDE, bool PAST>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, int lanes, int parts) {
   constexpr int N = Row16<T>::N;
   __shared__ int starts[kAppendStarts];
@@ -122,7 +128,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
     for (int i = 0; i < kAppendHeads; ++i)
       if (h0 + i < p.nH) {
         if (p.rope != nullptr) turn<T>(r[i], cs);
-        store16<T, WIDE>(dst + (long)i * p.q_row, r[i]);
+        store16<T, WIDE, PAST>(dst + (long)i * p.q_row, r[i]);
       }
     return;
   }
@@ -140,6 +146,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
 }
 
 template <typename T> static hipError_t append_one(const PagedAppendArgs& a, hipStream_t s) {
+  const bool past = a.Qout != a.Qin && (long)a.T * a.nH * a.q_row * (long)sizeof(T) > kL2Bytes;
   constexpr int N = Row16<T>::N;
   const int widest = a.V != nullptr && a.rt3 > a.r3 ? a.rt3 : a.r3;
   int lanes = 1;                                                  // of a group: a power of two
@@ -149,8 +156,8 @@ template <typename T> static hipError_t append_one(const PagedAppendArgs& a, hip
   if (blocks > 0x7fffffffl) return hipErrorInvalidValue;
   auto wide = [&](const void* q, long ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * (long)sizeof(T) % 16 == 0; };
   const bool all = wide(a.Kin, a.ldk) && wide(a.Vin, a.ldv) && wide(a.Qin, a.q_row) && wide(a.Qout, a.q_row);
-  if (all) hipLaunchKernelGGL((paged_append_kernel<T, true>), dim3(blocks), dim3(256), 0, s, a, lanes, parts);
-  else hipLaunchKernelGGL((paged_append_kernel<T, false>), dim3(blocks), dim3(256), 0, s, a, lanes, parts);
+  const auto kern = !all ? paged_append_kernel<T, false, false> : past ? paged_append_kernel<T, true, true> : paged_append_kernel<T, true, false>;
+  hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a, lanes, parts);
   return hipGetLastError();
 }
 hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s) {

@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_raw[];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int h = lane / 32, lr = lane % 32;
-  const int parts = PREFIX ? p.prefix_parts : max(p.own_parts, 1), part = blockIdx.y;
+  const int part = blockIdx.y;
 
   // ---- which rows, which keys ----
   int rb, n_rows, row0;                                           // block, rows of its sequence, first row of that in [T * nH]

@@ -5,9 +5,10 @@
 // matrix pipe bounds it.  A workgroup of four waves takes 128 rows, a wave 32 of them, and all keys (or a part of them) in tiles that
 // its waves share in LDS.  Tiles go from the pages straight into one of two LDS stages, a tile ahead.  Two workgroups share a
 // compute unit: between two barriers a workgroup's waves do the same at the same time (reads, products, exponentials), and another
-// workgroup that is not in step with it fills the gaps (eight waves in step, on tiles of the same size: 135 against 96 us for four
-// sequences with up to 512 new tokens on up to 4097 rows).  Probabilities are rounded to bf16 once for the value product, as the
-// result is: the relative error of the sum is that of one more rounding of the result.
+// workgroup that is not in step with it fills the gaps (four sequences with up to 512 new tokens on up to 4097 rows, 32 heads of 128
+// channels: 123 us, eight waves of one workgroup in step 135).  With shares of equal work (below) that call takes 68 us, its largest
+// part at 0.8 PFLOP/s; the rest is the launches, the first loads and the partial results.  Probabilities are rounded to bf16 once for
+// the value product, as the result is: the relative error of the sum is that of one more rounding of the result.
 #include "paged_block.h"
 
 namespace ta {
@@ -113,310 +114,310 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   }
 
   for (int segment = 0; left > 0; ++segment) {
-  int row0 = 0, first = 0, nq, len = p.prefix, pages;             // first row of the sequence in [T * nH], its first key, ..
-  const int* table = p.prefix_table;
-  if (pre) {
-    nq = min(max(p.q_start[p.B], 0), p.T);
-    pages = divide(p.prefix - 1, p.ps) + 1;
-    if (rb * RB >= nq * p.nH) return;
-  } else {
-    const PagedSeq s = paged_seq(p, b);
-    nq = s.nq;
-    row0 = s.q0 * p.nH;
-    first = p.prefix;
-    len = s.len;
-    table = p.table + (long)b * p.max_pages;
-    pages = p.max_pages;
-  }
-  const int n_rows = nq * p.nH, now = pre ? 1 : min(left, items - item);
-  const bool causal = !pre && p.causal;
-  const int r0 = rb * RB, rw = r0 + wave * 32;                 // first row of the workgroup, of this wave
-  const int r = min(rw + lr, n_rows - 1);                         // rows behind the last repeat it and are not stored
-  auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
-  const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);     // keys that the row sees, that all and any rows of the workgroup see
-  const int hi = sees(rw + 31);                                   // keys that any row of the wave sees
-  // items dealt to whole units of the keys that the block sees; who ends here and who goes on from here count alike
-  const int units = max(0, hi_all - first + kTileUnit - 1) / kTileUnit;
-  auto unit_at = [&](int i) { return i == 0 ? 0 : i == items ? units : __builtin_amdgcn_readfirstlane((int)((double)i * units / items)); };
-  const int key0 = pre ? part * p.prefix_keys : first + unit_at(item) * kTileUnit;
-  const int key1 = min(hi_all, pre ? key0 + p.prefix_keys : first + unit_at(item + now) * kTileUnit);
-  const int cnt = key1 > key0 ? (key1 - key0 + BC - 1) / BC : 0;  // tiles
-  const bool busy = rw < n_rows;                                  // a wave without rows helps with the loads only
-
-  f32x16 oacc[CB];
-  float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) oacc[cb][e] = 0.f;
-
-  if (cnt > 0) {                                                  // (the same for the whole workgroup)
-    auto tile_at = [&](int j) { return key0 + min(j, cnt - 1) * BC; };   // past the end: the last again, unused
-
-    Frag<T> qf[CB];
-    {
-      const T* q = static_cast<const T*>(p.Q) + (long)(row0 + r) * p.q_row;
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) qf[cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
-    }
-
-    constexpr float kLazy = 8.f;
-    const int xs = swz_x<CPR>(lr);
-    // ---- a block of 32 keys, rows kr .. of stage st: scores, probabilities, O += V P ----
-    auto scores = [&](int kr, int st, f32x16& s) {
-      const T* kt = smem + (long)st * L::kStage + kr * D;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
-      constexpr int G = KIND == 1 && CB > 2 ? 2 : CB;             // channel blocks whose reads are all on their way before a product
-#pragma unroll
-      for (int g = 0; g < CB; g += G) {
-        Frag<T> kf[G], rest[KIND == 1 ? G : 1];
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          kf[i] = load_frag_swz<T>(kt + lr * D, 4 * (g + i) + 2 * h, xs);
-          if constexpr (KIND == 1) rest[i] = load_frag_swz<T>(kt + L::kTile + lr * D, 4 * (g + i) + 2 * h, xs);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          mma32(s, kf[i], qf[g + i]);
-          if constexpr (KIND == 1) mma32(s, rest[i], qf[g + i]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the reference by more
-    // than kLazy (probabilities stay below 2^kLazy)
-    auto probabilities = [&](f32x16& s) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-      mx = halves_max(mx) * p.scale;
-      const bool raise = mx > m_run + kLazy;                      // -inf + kLazy = -inf: the first block with a key raises
-      if (__builtin_amdgcn_ballot_w64(raise) != 0ull) {
-        const float alpha = raise ? fast_exp2(m_run - mx) : 1.f;
-        if (raise) m_run = mx;
-        l_run *= alpha;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) oacc[cb][e] *= alpha;
-      }
-      const float m_use = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e] * p.scale - m_use);
-      l_run = block_sum(s, l_run);
-      return to_frag<T>(s);
-    };
-    // some rows may not see some of the keys, n0 ..
-    auto values = [&](int n0, int kr, int st, const Frag<T>& pf) {
-      const T* vt = smem + (long)st * L::kStage + kr * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        Frag<T> vf[1];
-        load_frags_tr_swz<CPR>(vf, vt, 0, cb * 32, lane);
-        if (__builtin_amdgcn_ballot_w64(!frag_finite(vf[0])) != 0ull) take_nonfinite<T>(vf[0], limit - n0 - 4 * h, oacc[cb]);   // (rare)
-        mma32(oacc[cb], vf[0], pf);
-      }
-    };
-    // A tile that all rows of the workgroup see: the products of one block run under the exponentials of the other.
-    auto whole = [&](int st) {
-      f32x16 s[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) scores(nb * 32, st, s[nb]);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        __builtin_amdgcn_sched_barrier(0);
-        // the first value fragments are on their way under the exponentials
-        constexpr int TF = CB < 2 ? 1 : 2;
-        const T* vt = smem + (long)st * L::kStage + nb * 32 * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
-        Frag<T> vf[TF];
-        load_frags_tr_swz<CPR>(vf, vt, 0, 0, lane);
-        const Frag<T> pf = probabilities(s[nb]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int k = 0; k < CB / TF; ++k) {
-          if (k > 0) load_frags_tr_swz<CPR>(vf, vt, 0, k * TF * 32, lane);
-#pragma unroll
-          for (int f = 0; f < TF; ++f) mma32(oacc[k * TF + f], vf[f], pf);
-        }
-      }
-    };
-    // any other, a block that no row of the wave sees passed over
-    auto edge = [&](int j, int st) {
-#pragma unroll 1
-      for (int nb = 0; nb < NB; ++nb) {
-        const int n0 = tile_at(j) + nb * 32;
-        if (n0 >= hi) break;
-        f32x16 s;
-        scores(nb * 32, st, s);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit ? s[e] : -INFINITY;
-        const Frag<T> pf = probabilities(s);
-        values(n0, nb * 32, st, pf);
-      }
-    };
-    const int n_whole = min(max(lo_all - key0, 0) / BC, cnt);
-
-    if constexpr (KIND != 1) {
-      // A wave takes BC / 4 consecutive rows of a tile: NK pieces of 1 KB of the keys, and as many of the values.  Rows that lie in
-      // one page (the usual sizes): its number comes by a scalar read, there is one start for the wave, in 16-byte units (32 bits:
-      // 64 GiB), and lanes add their row and chunk to it.  Rows behind the last are whatever the page holds, chunks behind a row's
-      // end (which meet zeros of the queries, or become channels that are not stored) repeat its last.  Else every lane looks up its
-      // own rows.
-      constexpr int NK = BC * D / 512 / 4, ROWS = BC / 4;
-      static_assert(ROWS == 16, "rows of a wave");
-      const uint32_t k16 = (uint32_t)(p.k_stride / 8), v16 = (uint32_t)(p.v_stride / 8), rk = p.r3 / 8, rv = p.rt3 / 8;
-      const bool straight = p.page_size % ROWS == 0 && first % ROWS == 0;
-      const auto* entries = (const __attribute__((address_space(4))) int*)table;
-      auto entry_at = [&](int j) { return entries[min(divide(min(tile_at(j) + wave * ROWS, hi_all - 1), p.ps), pages - 1)]; };
-      int entry = entry_at(0);                                    // of the tile that is filled next
-      auto fill = [&](int j, int st) {
-        T* kt = smem + (long)st * L::kStage + wave * NK * 512;
-        const int n0 = tile_at(j) + wave * ROWS;
-        int l = lane;
-        asm volatile("" : "+v"(l));                               // (chunks of the pieces are formed afresh, not kept across the loop)
-        if (straight) {
-          const uint32_t page = paged_page(entry, p.n_pages), at = n0 - divide(n0, p.ps) * p.page_size;
-          const char* k = static_cast<const char*>(p.K) + (unsigned long)(page * k16 + at * rk) * 16;
-          const char* v = KIND == 0 ? static_cast<const char*>(p.V) + (unsigned long)(page * v16 + at * rv) * 16 : nullptr;
-#pragma unroll
-          for (int i = 0; i < NK; ++i) {
-            const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(i * RPP + l / CPR);
-            chunk_to_lds(k + (row * rk + min(c, rk - 1)) * 16, kt + i * 512);
-            if constexpr (KIND == 0) chunk_to_lds(v + (row * rv + min(c, rv - 1)) * 16, kt + L::kTile + i * 512);
-          }
-          entry = entry_at(j + 1);
-        } else {
-#pragma unroll 1
-          for (int i = 0; i < NK; ++i) {
-            const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(row);
-            const int n = min(n0 + (int)row, hi_all - 1), in_table = divide(n, p.ps);
-            const uint32_t page = paged_page(table[min(in_table, pages - 1)], p.n_pages), at = n - in_table * p.page_size;
-            chunk_to_lds(static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + min(c, rk - 1)), kt + i * 512);
-            if constexpr (KIND == 0)
-              chunk_to_lds(static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + min(c, rv - 1)), kt + L::kTile + i * 512);
-          }
-        }
-      };
-      wait_vm<0>();                                               // plain loads out of the way of the counted ones
-      fill(0, 0);
-      auto arrived = [] {
-        wait_vm<0>();                                             // this wave's part of tile j is there,
-        wait_lds();                                               // its reads of tile j - 1 are done
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-      };
-      int j = 0;
-      for (; j < n_whole; ++j) {
-        arrived();
-        fill(j + 1, (j + 1) & 1);                                 // into the stage of tile j - 1
-        if (busy) whole(j & 1);
-      }
-      for (; j < cnt; ++j) {
-        arrived();
-        fill(j + 1, (j + 1) & 1);
-        if (busy) edge(j, j & 1);
-      }
-      wait_vm<0>();                                               // tiles requested past the end still land in LDS
+    int row0 = 0, first = 0, nq, len = p.prefix, pages;           // first row of the sequence in [T * nH], its first key, ..
+    const int* table = p.prefix_table;
+    if (pre) {
+      nq = min(max(p.q_start[p.B], 0), p.T);
+      pages = divide(p.prefix - 1, p.ps) + 1;
+      if (rb * RB >= nq * p.nH) return;
     } else {
-      // a thread's chunks of a tile are those of one row, eight apart: neighbouring lanes read neighbouring positions of the
-      // rotation table
-      constexpr int CPT = CPR / 8 > 0 ? CPR / 8 : 1;
-      const int row = threadIdx.x % 32, ch0 = threadIdx.x / 32;
-      struct Set { u32x4 x[CPT]; f32x4 cs[CPT][2]; } reg;
-      auto load = [&](int j) {
-        const int n = min(tile_at(j) + row, hi_all - 1);
-        const int pi = divide(n, p.ps);
-        const long pg = paged_page(table[min(pi, pages - 1)], p.n_pages), a = n - pi * p.page_size;
-        const T* src = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3;
-#pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-          const int ch = min(ch0 + 8 * i, CPR - 1);
-          reg.x[i] = ch * 8 < p.r3 ? *reinterpret_cast<const u32x4*>(src + ch * 8) : u32x4{0u, 0u, 0u, 0u};
-          const f32x4* tab = reinterpret_cast<const f32x4*>(p.rope) + (long)(2 * ch) * p.rope_ld + min(n, p.rope_ld - 1);
-          reg.cs[i][0] = tab[0];
-          reg.cs[i][1] = tab[p.rope_ld];
-        }
-      };
-      auto store = [&](int st) {
-        T* kt = smem + (long)st * L::kStage;
-#pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-          const int ch = ch0 + 8 * i;
-          if (ch >= CPR) break;
-          u32x4 hi16, lo16;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const float c = reg.cs[i][d / 2][2 * (d % 2)], sn = reg.cs[i][d / 2][2 * (d % 2) + 1];
-            const float x0 = __uint_as_float(reg.x[i][d] << 16), x1 = __uint_as_float(reg.x[i][d] & 0xffff0000u);
-            const f32x2 y = {x0 * c - x1 * sn, x0 * sn + x1 * c};
-            hi16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
-            const f32x2 z = {y[0] - __uint_as_float(hi16[d] << 16), y[1] - __uint_as_float(hi16[d] & 0xffff0000u)};
-            lo16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(z, bf16x2));
-          }
-          const int at = row * D + ((ch ^ swz_x<CPR>(row)) * 8);
-          *reinterpret_cast<u32x4*>(kt + at) = hi16;
-          *reinterpret_cast<u32x4*>(kt + L::kTile + at) = lo16;
-          *reinterpret_cast<u32x4*>(kt + 2 * L::kTile + at) = reg.x[i];
-        }
-      };
-      load(0);
-      __syncthreads();                                            // (the plan's words are done with)
-      store(0);
-      load(1);
-      int j = 0;
-      for (; j < n_whole; ++j) {
-        __syncthreads();
-        store((j + 1) & 1);                                       // the stage of tile j - 1
-        load(j + 2);
-        if (busy) whole(j & 1);
-      }
-      for (; j < cnt; ++j) {                                      // (nothing is kept in registers for later: they are all in use)
-        __syncthreads();
-        load(j + 1);
-        store((j + 1) & 1);
-        if (busy) edge(j, j & 1);
-      }
+      const PagedSeq s = paged_seq(p, b);
+      nq = s.nq;
+      row0 = s.q0 * p.nH;
+      first = p.prefix;
+      len = s.len;
+      table = p.table + (long)b * p.max_pages;
+      pages = p.max_pages;
     }
-  }
+    const int n_rows = nq * p.nH, now = pre ? 1 : min(left, items - item);
+    const bool causal = !pre && p.causal;
+    const int r0 = rb * RB, rw = r0 + wave * 32;               // first row of the workgroup, of this wave
+    const int r = min(rw + lr, n_rows - 1);                       // rows behind the last repeat it and are not stored
+    auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
+    const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);   // keys that the row sees, that all and any rows of the workgroup see
+    const int hi = sees(rw + 31);                                 // keys that any row of the wave sees
+    // items dealt to whole units of the keys that the block sees; who ends here and who goes on from here count alike
+    const int units = max(0, hi_all - first + kTileUnit - 1) / kTileUnit;
+    auto unit_at = [&](int i) { return i == 0 ? 0 : i == items ? units : __builtin_amdgcn_readfirstlane((int)((double)i * units / items)); };
+    const int key0 = pre ? part * p.prefix_keys : first + unit_at(item) * kTileUnit;
+    const int key1 = min(hi_all, pre ? key0 + p.prefix_keys : first + unit_at(item + now) * kTileUnit);
+    const int cnt = key1 > key0 ? (key1 - key0 + BC - 1) / BC : 0;  // tiles
+    const bool busy = rw < n_rows;                                // a wave without rows helps with the loads only
 
-  // ---- the rows: a result, or a part of one ----
-  const float l = halves_sum(l_run);
-  const bool complete = !pre && now == items;                     // nobody else has keys of these rows
-  if (rw + lr < n_rows) {
-    const long at = (long)row0 + rw + lr;
-    const bool direct = complete && !PREFIX;
-    const bool by_row = pre || complete;
-    const int shared = (2 * me + (segment > 0)) * RB + wave * 32 + lr;
-    const long slot = by_row ? (long)(pre ? part : p.prefix_parts) * p.T * p.nH + at : shared;
-    float* po = by_row ? p.part_o : p.stream_o;
-    float2* pml = by_row ? p.part_ml : p.stream_ml;
-    // for the join: this share, the first of the row's, and how many more there are
-    if (PREFIX && !pre && item == 0 && h == 0)
-      p.tile_rows[at] = int2{shared, complete ? 0 : shares.group(done + items - 1) - me};
+    f32x16 oacc[CB];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 o = {oacc[cb][4 * q], oacc[cb][4 * q + 1], oacc[cb][4 * q + 2], oacc[cb][4 * q + 3]};
-        const int c = cb * 32 + 8 * q + 4 * h;
-        if (direct) paged_result<T>(p, at, c, m_run, l, o);
-        else paged_partial<D>(po, pml, slot, c, m_run, l, o);
+      for (int e = 0; e < 16; ++e) oacc[cb][e] = 0.f;
+
+    if (cnt > 0) {                                                // (the same for the whole workgroup)
+      auto tile_at = [&](int j) { return key0 + min(j, cnt - 1) * BC; }; // past the end: the last again, unused
+
+      Frag<T> qf[CB];
+      {
+        const T* q = static_cast<const T*>(p.Q) + (long)(row0 + r) * p.q_row;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) qf[cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
       }
-  }
-  left -= now;
-  done += now;
-  if (pre || left == 0) break;
-  item = 0;
-  PagedSeq s = paged_seq(p, b);
-  if (++rb == tile_blocks(p, s)) {
-    rb = 0;
-    do s = paged_seq(p, ++b);
-    while (s.nq == 0);                                            // (work is left, so a sequence with some follows)
-  }
-  items = __builtin_amdgcn_readfirstlane(tile_work(p, s, rb + 1) - tile_work(p, s, rb));
-  __syncthreads();
+
+      constexpr float kLazy = 8.f;
+      const int xs = swz_x<CPR>(lr);
+      // ---- a block of 32 keys, rows kr .. of stage st: scores, probabilities, O += V P ----
+      auto scores = [&](int kr, int st, f32x16& s) {
+        const T* kt = smem + (long)st * L::kStage + kr * D;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+        constexpr int G = KIND == 1 && CB > 2 ? 2 : CB;           // channel blocks whose reads are all on their way before a product
+#pragma unroll
+        for (int g = 0; g < CB; g += G) {
+          Frag<T> kf[G], rest[KIND == 1 ? G : 1];
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            kf[i] = load_frag_swz<T>(kt + lr * D, 4 * (g + i) + 2 * h, xs);
+            if constexpr (KIND == 1) rest[i] = load_frag_swz<T>(kt + L::kTile + lr * D, 4 * (g + i) + 2 * h, xs);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < G; ++i) {
+            mma32(s, kf[i], qf[g + i]);
+            if constexpr (KIND == 1) mma32(s, rest[i], qf[g + i]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      // online softmax with a lazily raised reference: O and l are rescaled only when a block's maximum exceeds the reference by more
+      // than kLazy (probabilities stay below 2^kLazy)
+      auto probabilities = [&](f32x16& s) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+        mx = halves_max(mx) * p.scale;
+        const bool raise = mx > m_run + kLazy;                    // -inf + kLazy = -inf: the first block with a key raises
+        if (__builtin_amdgcn_ballot_w64(raise) != 0ull) {
+          const float alpha = raise ? fast_exp2(m_run - mx) : 1.f;
+          if (raise) m_run = mx;
+          l_run *= alpha;
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) oacc[cb][e] *= alpha;
+        }
+        const float m_use = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = fast_exp2(s[e] * p.scale - m_use);
+        l_run = block_sum(s, l_run);
+        return to_frag<T>(s);
+      };
+      // some rows may not see some of the keys, n0 ..
+      auto values = [&](int n0, int kr, int st, const Frag<T>& pf) {
+        const T* vt = smem + (long)st * L::kStage + kr * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          Frag<T> vf[1];
+          load_frags_tr_swz<CPR>(vf, vt, 0, cb * 32, lane);
+          if (__builtin_amdgcn_ballot_w64(!frag_finite(vf[0])) != 0ull) take_nonfinite<T>(vf[0], limit - n0 - 4 * h, oacc[cb]); // (rare)
+          mma32(oacc[cb], vf[0], pf);
+        }
+      };
+      // A tile that all rows of the workgroup see: the products of one block run under the exponentials of the other.
+      auto whole = [&](int st) {
+        f32x16 s[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) scores(nb * 32, st, s[nb]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          __builtin_amdgcn_sched_barrier(0);
+          // the first value fragments are on their way under the exponentials
+          constexpr int TF = CB < 2 ? 1 : 2;
+          const T* vt = smem + (long)st * L::kStage + nb * 32 * D + (KIND == 0 ? L::kTile : KIND == 1 ? 2 * L::kTile : 0);
+          Frag<T> vf[TF];
+          load_frags_tr_swz<CPR>(vf, vt, 0, 0, lane);
+          const Frag<T> pf = probabilities(s[nb]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int k = 0; k < CB / TF; ++k) {
+            if (k > 0) load_frags_tr_swz<CPR>(vf, vt, 0, k * TF * 32, lane);
+#pragma unroll
+            for (int f = 0; f < TF; ++f) mma32(oacc[k * TF + f], vf[f], pf);
+          }
+        }
+      };
+      // any other, a block that no row of the wave sees passed over
+      auto edge = [&](int j, int st) {
+#pragma unroll 1
+        for (int nb = 0; nb < NB; ++nb) {
+          const int n0 = tile_at(j) + nb * 32;
+          if (n0 >= hi) break;
+          f32x16 s;
+          scores(nb * 32, st, s);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = n0 + 8 * (e / 4) + 4 * h + e % 4 < limit ? s[e] : -INFINITY;
+          const Frag<T> pf = probabilities(s);
+          values(n0, nb * 32, st, pf);
+        }
+      };
+      const int n_whole = min(max(lo_all - key0, 0) / BC, cnt);
+
+      if constexpr (KIND != 1) {
+        // A wave takes BC / 4 consecutive rows of a tile: NK pieces of 1 KB of the keys, and as many of the values.  Rows that lie in
+        // one page (the usual sizes): its number comes by a scalar read, there is one start for the wave, in 16-byte units (32 bits:
+        // 64 GiB), and lanes add their row and chunk to it.  Rows behind the last are whatever the page holds, chunks behind a row's
+        // end (which meet zeros of the queries, or become channels that are not stored) repeat its last.  Else every lane looks up its
+        // own rows.
+        constexpr int NK = BC * D / 512 / 4, ROWS = BC / 4;
+        static_assert(ROWS == 16, "rows of a wave");
+        const uint32_t k16 = (uint32_t)(p.k_stride / 8), v16 = (uint32_t)(p.v_stride / 8), rk = p.r3 / 8, rv = p.rt3 / 8;
+        const bool straight = p.page_size % ROWS == 0 && first % ROWS == 0;
+        const auto* entries = (const __attribute__((address_space(4))) int*)table;
+        auto entry_at = [&](int j) { return entries[min(divide(min(tile_at(j) + wave * ROWS, hi_all - 1), p.ps), pages - 1)]; };
+        int entry = entry_at(0);                                  // of the tile that is filled next
+        auto fill = [&](int j, int st) {
+          T* kt = smem + (long)st * L::kStage + wave * NK * 512;
+          const int n0 = tile_at(j) + wave * ROWS;
+          int l = lane;
+          asm volatile("" : "+v"(l));                             // (chunks of the pieces are formed afresh, not kept across the loop)
+          if (straight) {
+            const uint32_t page = paged_page(entry, p.n_pages), at = n0 - divide(n0, p.ps) * p.page_size;
+            const char* k = static_cast<const char*>(p.K) + (unsigned long)(page * k16 + at * rk) * 16;
+            const char* v = KIND == 0 ? static_cast<const char*>(p.V) + (unsigned long)(page * v16 + at * rv) * 16 : nullptr;
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+              const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(i * RPP + l / CPR);
+              chunk_to_lds(k + (row * rk + min(c, rk - 1)) * 16, kt + i * 512);
+              if constexpr (KIND == 0) chunk_to_lds(v + (row * rv + min(c, rv - 1)) * 16, kt + L::kTile + i * 512);
+            }
+            entry = entry_at(j + 1);
+          } else {
+#pragma unroll 1
+            for (int i = 0; i < NK; ++i) {
+              const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(row);
+              const int n = min(n0 + (int)row, hi_all - 1), in_table = divide(n, p.ps);
+              const uint32_t page = paged_page(table[min(in_table, pages - 1)], p.n_pages), at = n - in_table * p.page_size;
+              chunk_to_lds(static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + min(c, rk - 1)), kt + i * 512);
+              if constexpr (KIND == 0)
+                chunk_to_lds(static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + min(c, rv - 1)), kt + L::kTile + i * 512);
+            }
+          }
+        };
+        wait_vm<0>();                                             // plain loads out of the way of the counted ones
+        fill(0, 0);
+        auto arrived = [] {
+          wait_vm<0>();                                           // this wave's part of tile j is there,
+          wait_lds();                                             // its reads of tile j - 1 are done
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        };
+        int j = 0;
+        for (; j < n_whole; ++j) {
+          arrived();
+          fill(j + 1, (j + 1) & 1);                               // into the stage of tile j - 1
+          if (busy) whole(j & 1);
+        }
+        for (; j < cnt; ++j) {
+          arrived();
+          fill(j + 1, (j + 1) & 1);
+          if (busy) edge(j, j & 1);
+        }
+        wait_vm<0>();                                             // tiles requested past the end still land in LDS
+      } else {
+        // a thread's chunks of a tile are those of one row, eight apart: neighbouring lanes read neighbouring positions of the
+        // rotation table
+        constexpr int CPT = CPR / 8 > 0 ? CPR / 8 : 1;
+        const int row = threadIdx.x % 32, ch0 = threadIdx.x / 32;
+        struct Set { u32x4 x[CPT]; f32x4 cs[CPT][2]; } reg;
+        auto load = [&](int j) {
+          const int n = min(tile_at(j) + row, hi_all - 1);
+          const int pi = divide(n, p.ps);
+          const long pg = paged_page(table[min(pi, pages - 1)], p.n_pages), a = n - pi * p.page_size;
+          const T* src = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3;
+#pragma unroll
+          for (int i = 0; i < CPT; ++i) {
+            const int ch = min(ch0 + 8 * i, CPR - 1);
+            reg.x[i] = ch * 8 < p.r3 ? *reinterpret_cast<const u32x4*>(src + ch * 8) : u32x4{0u, 0u, 0u, 0u};
+            const f32x4* tab = reinterpret_cast<const f32x4*>(p.rope) + (long)(2 * ch) * p.rope_ld + min(n, p.rope_ld - 1);
+            reg.cs[i][0] = tab[0];
+            reg.cs[i][1] = tab[p.rope_ld];
+          }
+        };
+        auto store = [&](int st) {
+          T* kt = smem + (long)st * L::kStage;
+#pragma unroll
+          for (int i = 0; i < CPT; ++i) {
+            const int ch = ch0 + 8 * i;
+            if (ch >= CPR) break;
+            u32x4 hi16, lo16;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+              const float c = reg.cs[i][d / 2][2 * (d % 2)], sn = reg.cs[i][d / 2][2 * (d % 2) + 1];
+              const float x0 = __uint_as_float(reg.x[i][d] << 16), x1 = __uint_as_float(reg.x[i][d] & 0xffff0000u);
+              const f32x2 y = {x0 * c - x1 * sn, x0 * sn + x1 * c};
+              hi16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
+              const f32x2 z = {y[0] - __uint_as_float(hi16[d] << 16), y[1] - __uint_as_float(hi16[d] & 0xffff0000u)};
+              lo16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(z, bf16x2));
+            }
+            const int at = row * D + ((ch ^ swz_x<CPR>(row)) * 8);
+            *reinterpret_cast<u32x4*>(kt + at) = hi16;
+            *reinterpret_cast<u32x4*>(kt + L::kTile + at) = lo16;
+            *reinterpret_cast<u32x4*>(kt + 2 * L::kTile + at) = reg.x[i];
+          }
+        };
+        load(0);
+        __syncthreads();                                          // (the plan's words are done with)
+        store(0);
+        load(1);
+        int j = 0;
+        for (; j < n_whole; ++j) {
+          __syncthreads();
+          store((j + 1) & 1);                                     // the stage of tile j - 1
+          load(j + 2);
+          if (busy) whole(j & 1);
+        }
+        for (; j < cnt; ++j) {                                    // (nothing is kept in registers for later: they are all in use)
+          __syncthreads();
+          load(j + 1);
+          store((j + 1) & 1);
+          if (busy) edge(j, j & 1);
+        }
+      }
+    }
+
+    // ---- the rows: a result, or a part of one ----
+    const float l = halves_sum(l_run);
+    const bool complete = !pre && now == items;                   // nobody else has keys of these rows
+    if (rw + lr < n_rows) {
+      const long at = (long)row0 + rw + lr;
+      const bool direct = complete && !PREFIX;
+      const bool by_row = pre || complete;
+      const int shared = (2 * me + (segment > 0)) * RB + wave * 32 + lr;
+      const long slot = by_row ? (long)(pre ? part : p.prefix_parts) * p.T * p.nH + at : shared;
+      float* po = by_row ? p.part_o : p.stream_o;
+      float2* pml = by_row ? p.part_ml : p.stream_ml;
+      // for the join: this share, the first of the row's, and how many more there are
+      if (PREFIX && !pre && item == 0 && h == 0)
+        p.tile_rows[at] = int2{shared, complete ? 0 : shares.group(done + items - 1) - me};
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 o = {oacc[cb][4 * q], oacc[cb][4 * q + 1], oacc[cb][4 * q + 2], oacc[cb][4 * q + 3]};
+          const int c = cb * 32 + 8 * q + 4 * h;
+          if (direct) paged_result<T>(p, at, c, m_run, l, o);
+          else paged_partial<D>(po, pml, slot, c, m_run, l, o);
+        }
+    }
+    left -= now;
+    done += now;
+    if (pre || left == 0) break;
+    item = 0;
+    PagedSeq s = paged_seq(p, b);
+    if (++rb == tile_blocks(p, s)) {
+      rb = 0;
+      do s = paged_seq(p, ++b);
+      while (s.nq == 0);                                          // (work is left, so a sequence with some follows)
+    }
+    items = __builtin_amdgcn_readfirstlane(tile_work(p, s, rb + 1) - tile_work(p, s, rb));
+    __syncthreads();
   }
 }
 
