@@ -299,8 +299,8 @@ int tucker_attn_append_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *page
                              const void *K, int64_t ldk, const void *V, int64_t ldv, const void *Q, void *Qrot,
                              int32_t rotate, void *hip_stream);
 
-/* Bytes of device workspace the two calls below need for a batch of these bounds (prefix_len 0: the first one); 0 if an argument
- * is invalid.  The arrays of the batch are not looked at. */
+/* Bytes of device workspace the two calls below need for a batch of these bounds (prefix_len 0: the first one); 0 if they need none,
+ * or an argument is invalid.  The arrays of the batch are not looked at. */
 size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tucker_attn_batch *batch, int32_t prefix_len);
 
 /*
@@ -348,7 +348,7 @@ int tucker_attn_forward_paged(tucker_attn_ctx *ctx, const tucker_attn_weights *w
                               int32_t prefix_len, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
- * Optional per-kernel timing for benchmarks.  While enabled, forward/backward/decode bracket every
+ * Optional per-kernel timing for benchmarks.  While enabled, forward/backward/decode and the calls over pages bracket every
  * kernel they launch with HIP events recorded on the caller's stream; tucker_attn_profile_read
  * synchronises those events and returns, for the LAST call, the kernel count and for each
  * kernel its name and duration (the time between the two events around the launch, which includes

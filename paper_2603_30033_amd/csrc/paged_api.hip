@@ -8,6 +8,12 @@ using namespace ta;
 
 namespace {
 
+// (no kernel here has events of its own: what a forward call left there is not this call's)
+hipError_t begin(Recorder& rec) {
+  if (rec.on) rec.c->kev_name = nullptr;
+  return rec.begin();
+}
+
 constexpr long kMaxRows = 1l << 31;   // (token, head) rows of a call
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -159,7 +165,7 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
   if (workspace_bytes < need) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
-  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (begin(rec) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   return launch_attend(c, a, s, rec);
 }
 
@@ -210,7 +216,7 @@ int tucker_attn_append_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages,
   a.rotate_k = rotate && !f.shared_kv;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
-  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (begin(rec) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   if (launch_paged_append(f.dtype, a, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("paged_append");
   return TUCKER_ATTN_OK;
@@ -258,7 +264,7 @@ int tucker_attn_forward_paged(tucker_attn_ctx* c, const tucker_attn_weights* w, 
 
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
-  if (rec.begin() != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
+  if (begin(rec) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   if (c->prepared) {
     Carver cv{static_cast<char*>(c->prepared), 0};
     carve_weights(c, cv, ws.Gt, ws.Gtil2, ws.Wcat, ws.Ut2p);

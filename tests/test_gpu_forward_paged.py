@@ -240,3 +240,16 @@ def test_equals_the_contiguous_cache():
         last = X[:, 64].contiguous()
         y = to_host(layer.forward_paged(last, pools, batch))
         check(y, to_host(layer.decode(last, Kc, Vc, [65, 65])), w.dtype, "against decode")
+
+
+def test_profiled_calls_name_their_own_kernels():
+    w, inp, _ = inputs(CASES["bf16"], B=2, N=64)
+    with Layer(w, inp, max_positions=64) as layer:
+        X = to_device(inp["X"], w.dtype)
+        ta.tucker_attn_profile_enable(layer.ctx, True)
+        layer.forward(X)
+        assert "attention_kernel" in dict(ta.tucker_attn_profile_read(layer.ctx))
+        s = Server(w, layer, 2, 16, pages=8)
+        s.step([X[0], X[1]], [64, 3])
+        names = [n for n, _ in ta.tucker_attn_profile_read(layer.ctx)]
+    assert names == ["prep_weights", "factor_projection", "head_queries", "paged_append", "paged_attention", "latent_merge", "output_projection"]

@@ -144,6 +144,51 @@ def test_many_sequences_and_a_long_one(dtype):
         check(c, b, *attend(c, b, *on_gpu(b)))
 
 
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("heads,r,B", [(32, 128, 128), (32, 128, 129), (12, 64, 140), (32, 128, 257), (3, 32, 300)])
+def test_a_step_of_many_sequences_of_hundreds_of_rows(heads, r, B, shared):
+    # around the number of sequences from which row blocks in place of sequences are dealt to the workgroups
+    rows = [1 + (53 * i) % 700 for i in range(B)]
+    b = Batch([int(i % 9 != 4) for i in range(B)], rows, 16, r, r, heads, torch.bfloat16, shared=shared, seed=B)
+    with Context(heads, r, r, "bf16", shared=shared) as c:
+        check(c, b, *attend(c, b, *on_gpu(b)))
+
+
+@pytest.mark.parametrize("heads,r3,rt3", [(32, 128, 128), (12, 64, 32), (1, 32, 32), (70, 64, 64), (130, 32, 32)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_whole_prompts(causal, heads, r3, rt3):
+    # row blocks that see from a few keys to all of them
+    new = [300, 0, 701, 40, 1]
+    b = Batch(new, new, 16, r3, rt3, heads, torch.bfloat16, seed=heads, padding=3)
+    with Context(heads, r3, rt3, "bf16", causal=causal) as c:
+        check(c, b, *attend(c, b, *on_gpu(b)), causal=causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("heads,r", [(12, 64), (32, 128), (3, 32)])
+@pytest.mark.parametrize("new,own", [([1, 3, 60, 0, 1], [1200, 700, 1900, 5, 1]), ([1] * 20, [1 + 90 * i for i in range(20)])])
+def test_many_own_keys_behind_a_prefix(new, own, heads, r, shared, dtype):
+    b = Batch(new, [70 + n for n in own], 16, r, r, heads, DT[dtype], shared=shared, prefix=70, seed=heads, padding=1)
+    with Context(heads, r, r, dtype, shared=shared) as c:
+        check(c, b, *attend(c, b, *on_gpu(b)))
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("heads,r", [(32, 128), (12, 64)])
+def test_what_a_token_behind_a_prefix_does_not_see_does_not_reach_it(heads, r, bad):
+    b = Batch([4, 1, 1], [510, 480, 433], 16, r, r, heads, torch.bfloat16, prefix=433, seed=17)
+    with Context(heads, r, r, "bf16") as c:
+        O, L = attend(c, b, *on_gpu(b))
+        at = b.rows_of(0)
+        b.K.view(-1, r)[at[-1]] = bad                             # rows of the last token of the first sequence only
+        b.V.view(-1, r)[at[-1]] = bad
+        O2, L2 = attend(c, b, *on_gpu(b))
+        others = [0, 1, 2, 4, 5]
+        assert torch.equal(O[others], O2[others]) and torch.equal(L[others], L2[others])
+        assert not torch.isfinite(O2[3].float()).any()
+
+
 @pytest.mark.parametrize("rows", [4096, 32768])
 def test_one_long_sequence(rows):
     b = Batch([1], [rows], 64, 128, 128, 32, torch.bfloat16, seed=9)
