@@ -10,7 +10,7 @@
 // for (8189 tokens of 32 heads of 128 channels: 37.1 us, looked for first 38.5; with 4, 16 heads a group 38.6, 45.0).  Rotated queries
 // that no L2 can hold until they are read go past the caches, which leaves these to what the call still has to read: the same call
 // 26 us (5.5 TB/s; a large copy has 4.9), together with the attention behind it 407 us for two prompts of 4096 tokens and 404
-// without.  Queries in place are in the caches already.  One token of 12 heads of 64 channels: 5.0 us, of which the launch is half.
+// without.  Queries in place are in the caches already.  One token of 12 heads of 64 channels: 5.0 us (a kernel that writes one element: 1.4).
 #include "paged.h"
 
 namespace ta {

@@ -155,14 +155,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs p, int group
   __shared__ float2 pml[SLOTS];
   const int tid = threadIdx.x, slot = tid / L, c = tid % L * 4, per = SLOTS / groups, group = slot / per;
   const long rows = (long)p.T * p.nH, row = (long)blockIdx.x * per + slot % per;
-  const int q0 = min(max(p.q_start[0], 0), p.T), q1 = min(max(p.q_start[p.B], 0), p.T);
-  const bool live = row >= (long)q0 * p.nH && row < (long)q1 * p.nH;   // not behind the last sequence
   RowSum sum;
-  if (live)
+  if (row < rows)
     sum.add_parts(p.prefix_parts + p.own_parts, group, groups, [&](int i, const float2*& ml, const float*& o) {
       ml = p.part_ml + i * rows + row;
       o = p.part_o + (i * rows + row) * D + c;
     });
+  const int q0 = min(max(p.q_start[0], 0), p.T), q1 = min(max(p.q_start[p.B], 0), p.T);
+  const bool live = row >= (long)q0 * p.nH && row < (long)q1 * p.nH;   // not behind the last sequence
   sum.add_groups(po, pml, slot, group, groups, per, L);
   if (group == 0 && live) paged_result<float>(p, row, c, sum.m, sum.l, sum.o);
 }

@@ -329,10 +329,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs p, int groups
   __shared__ float2 pml[SLOTS];
   const int b = blockIdx.x, tid = threadIdx.x;
   const PagedSeq s = paged_seq(p, b);
+  const int2 parts = p.stream_parts[b];                           // (of a sequence without a new token: anything)
   const int n_rows = s.nq * p.nH, per = SLOTS / groups;
-  if ((int)blockIdx.y * per >= n_rows) return;
-  const int2 parts = p.stream_parts[b];
-  if (parts.y == 1) return;                                       // one workgroup did it all and has written the result
+  if ((int)blockIdx.y * per >= n_rows || parts.y == 1) return;    // one workgroup did it all and has written the result
   const int slot = tid / L, c = tid % L * 4, group = slot / per, r = (int)blockIdx.y * per + slot % per;
   RowSum sum;
   if (r < n_rows)

@@ -155,11 +155,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       auto tile_at = [&](int j) { return key0 + min(j, cnt - 1) * BC; }; // past the end: the last again, unused
 
       Frag<T> qf[CB];
-      {
+      auto load_queries = [&] {
         const T* q = static_cast<const T*>(p.Q) + (long)(row0 + r) * p.q_row;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) qf[cb] = load_frag_upto<T>(q, cb * 32 + 16 * h, p.r3);
-      }
+      };
 
       constexpr float kLazy = 8.f;
       const int xs = swz_x<CPR>(lr);
@@ -300,8 +300,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
           }
         };
-        wait_vm<0>();                                             // plain loads out of the way of the counted ones
         fill(0, 0);
+        load_queries();                                           // (behind the first tile, whose way is the longer one)
         auto arrived = [] {
           wait_vm<0>();                                           // this wave's part of tile j is there,
           wait_lds();                                             // its reads of tile j - 1 are done
@@ -363,6 +363,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           }
         };
         load(0);
+        load_queries();
         __syncthreads();                                          // (the plan's words are done with)
         store(0);
         load(1);
@@ -442,28 +443,29 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int g
     row = (long)blockIdx.x * per + slot % per;
     const int q0 = min(max(p.q_start[0], 0), p.T), q1 = min(max(p.q_start[p.B], 0), p.T);
     live = row >= (long)q0 * p.nH && row < (long)q1 * p.nH;       // not behind the last sequence
-    const int2 e = live ? p.tile_rows[row] : int2{0, 0};
-    // (bounded: a row that no sequence has, where q_start says less than it should, finds anything here)
+    const int2 e = row < rows ? p.tile_rows[row] : int2{0, 0};
+    // (bounded: a row that no sequence has finds anything here)
     first = min(max(e.x, 0), max(2 * p.tile_wgs * kTileRows - 1, 0));
     more = min(max(e.y, 0), max(p.tile_wgs - 1 - first / (2 * kTileRows), 0));
   } else {
-    const int g = (int)blockIdx.x + 1, r = (int)blockIdx.y * per + slot % per;
-    if (g >= p.tile_cuts[0].x) return;
+    const int g = (int)blockIdx.x + 1, r = (int)blockIdx.y * per + slot % per, shares = p.tile_cuts[0].x;
     const int4 e = p.tile_cuts[g];
-    if ((int)blockIdx.y * per >= e.y) return;
+    if (g >= shares || (int)blockIdx.y * per >= e.y) return;
     live = r < e.y;
     row = (long)e.x + r;
     first = (2 * (g - 1) + e.w) * kTileRows + r;
     more = e.z - (g - 1);
   }
   RowSum sum;
-  if (live) {
-    if (PREFIX)
-      sum.add_parts(p.prefix_parts + (more == 0 ? 1 : 0), group, groups, [&](int i, const float2*& ml, const float*& o) {
-        ml = p.part_ml + i * rows + row;
-        o = p.part_o + (i * rows + row) * D + c;
-      });
-    if (more > 0)
+  if (PREFIX ? row < rows : live) {
+    auto by_row = [&](int i, const float2*& ml, const float*& o) {
+      ml = p.part_ml + i * rows + row;
+      o = p.part_o + (i * rows + row) * D + c;
+    };
+    if (PREFIX) sum.add_parts(p.prefix_parts, group, groups, by_row);   // (waits for nothing that is read above)
+    if (PREFIX && (more == 0 || !live))
+      sum.add_parts(1, group, groups, [&](int, const float2*& ml, const float*& o) { by_row(p.prefix_parts, ml, o); });
+    else
       sum.add_parts(more + 1, group, groups, [&](int i, const float2*& ml, const float*& o) {
         // share i's first segment, but the first share's last
         const long at = i == 0 ? first : (first / (2 * kTileRows) + i) * 2l * kTileRows + first % kTileRows;
