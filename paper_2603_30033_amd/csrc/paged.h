@@ -112,10 +112,10 @@ template <typename A> __device__ __forceinline__ PagedSeq paged_seq(const A& p, 
 // Page of a table entry; a number that is no page of the pool reads page 0
 __device__ __forceinline__ int paged_page(int entry, int n_pages) { return (uint32_t)entry < (uint32_t)n_pages ? entry : 0; }
 
-// Which sequence item `target` belongs to when every sequence has items(b) of them, one behind the other: its number (-1: behind
-// the last), the item's index in it, and the number of all items.  All 256 threads call; `sh` holds 6 words.
-template <class F>
-__device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh, int& index, int& total) {
+// Which sequence item target(total) belongs to when every sequence has items(b) of them, one behind the other, `total` together: the
+// sequence's number (-1: behind the last, or before the first), the item's index in it.  All 256 threads call; `sh` holds 6 words.
+template <class G, class F>
+__device__ __forceinline__ int paged_locate(int B, G target, F items, int* sh, int& index, int& total) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int per = (B + 255) / 256, first = tid * per, last = min(B, first + per);
   int mine = 0;
@@ -137,11 +137,13 @@ __device__ __forceinline__ int paged_locate(int B, int target, F items, int* sh,
     total += sh[w];
     before += w < wave ? sh[w] : 0;
   }
-  if (target >= before && target < before + mine) {
+  const int at = target(total);
+  if (at >= before && at < before + mine) {
     int b = first;
-    for (int n; target >= before + (n = items(b)); ++b) before += n;
+    if (per > 1)
+      for (int n; at >= before + (n = items(b)); ++b) before += n;
     sh[W] = b;
-    sh[W + 1] = target - before;
+    sh[W + 1] = at - before;
   }
   __syncthreads();
   index = sh[W + 1];

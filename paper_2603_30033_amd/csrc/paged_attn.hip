@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedArgs p) {
     if (rb * 32 >= n_rows) return;
   } else {
     int total;
-    const int b = paged_locate(p.B, blockIdx.x, [&](int i) { return (paged_seq(p, i).nq * p.nH + 31) / 32; },
+    const int b = paged_locate(p.B, [](int) { return (int)blockIdx.x; }, [&](int i) { return (paged_seq(p, i).nq * p.nH + 31) / 32; },
                                reinterpret_cast<int*>(smem_raw), rb, total);
     if (b < 0) return;
     const PagedSeq s = paged_seq(p, b);

@@ -40,15 +40,6 @@ __device__ __forceinline__ int block_total(int x, int* sh) {
   __syncthreads();
   return sh[0] + sh[1] + sh[2] + sh[3];
 }
-// Units of a workgroup where `mine` are thread i's sequence's (at most 256 sequences, and no more than half the workgroups): one round
-// of workgroups over the compute units, the units' share of each, or, where the sequences' last parts make too many of these, a share
-// that is larger by as much.
-__device__ __forceinline__ int stream_share(const PagedArgs& p, int mine, int* sh) {
-  const int all = block_total(mine, sh), units = max(kStreamLeast, (all + p.stream_wgs - 1) / p.stream_wgs);
-  if (block_total((mine + units - 1) / units, sh) <= p.stream_wgs) return units;
-  return max(units, (all + p.stream_wgs - p.B - 1) / (p.stream_wgs - p.B));
-}
-
 template <int D, int HB, int KIND>
 // Wide latents with two pools: LDS leaves one wave to a SIMD, which may then use all registers.  With one pool whose keys are rotated on
 // use the vector unit is busier than memory: two workgroups share a compute unit, and a stage is filled again at a round's end.
@@ -69,10 +60,19 @@ void paged_stream_kernel(PagedArgs p) {
     cnt = stream_units(p, b);
   } else {
     int* sh = reinterpret_cast<int*>(smem_raw);
-    const int mine = (int)threadIdx.x < p.B ? stream_units(p, threadIdx.x) : 0, units = stream_share(p, mine, sh);
-    int part, all;
+    // Units of a workgroup: one round of workgroups over the compute units, the units' share of each, or, where the sequences' last
+    // parts make too many of these, a share that is larger by as much.  (At most 256 sequences, thread i's is i, and no more than half
+    // the workgroups.)
+    const int mine = (int)threadIdx.x < p.B ? stream_units(p, threadIdx.x) : 0, n_all = block_total(mine, sh);
+    int units = max(kStreamLeast, (n_all + p.stream_wgs - 1) / p.stream_wgs), part, all;
+    auto me = [](int) { return (int)blockIdx.x; };
+    auto parts = [&](int) { return (mine + units - 1) / units; };
     __syncthreads();
-    b = paged_locate(p.B, blockIdx.x, [&](int) { return (mine + units - 1) / units; }, sh, part, all);   // (a sequence for every thread)
+    b = paged_locate(p.B, me, parts, sh, part, all);
+    if (all > p.stream_wgs) {
+      units = max(units, (n_all + p.stream_wgs - p.B - 1) / (p.stream_wgs - p.B));
+      b = paged_locate(p.B, me, parts, sh, part, all);
+    }
     if (b < 0) return;
     b = __builtin_amdgcn_readfirstlane(b);
     off = __builtin_amdgcn_readfirstlane(part) * units;

@@ -77,23 +77,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   } else {
     int index, all;
     if (p.tile_wgs == 0) {                                        // a workgroup for every row block
-      b = paged_locate(p.B, wg, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
+      b = paged_locate(p.B, [=](int) { return wg; }, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
       if (b < 0) return;
     } else {
-      auto work = [&](int i) { return tile_work(p, i); };
-      b = paged_locate(p.B, 0, work, reinterpret_cast<int*>(smem_raw), index, all);
+      auto start = [&](int total) {                               // of this workgroup's share; behind all if it has none
+        shares = Shares(total, p.tile_wgs, kTileLeast);
+        const int per = (shares.G + 7) / 8;
+        me = die * per + in_die;
+        return in_die < per && me < shares.G ? shares.first(me) : total;
+      };
+      b = paged_locate(p.B, start, [&](int i) { return tile_work(p, i); }, reinterpret_cast<int*>(smem_raw), index, all);
       if (b < 0) {
-        if (!PREFIX && blockIdx.x == 0 && threadIdx.x == 0) p.tile_cuts[0].x = 0;
+        if (!PREFIX && all == 0 && blockIdx.x == 0 && threadIdx.x == 0) p.tile_cuts[0].x = 0;
         return;
       }
-      const Shares sh(all, p.tile_wgs, kTileLeast);
-      const int per = (sh.G + 7) / 8;
-      me = die * per + in_die;
-      if (in_die >= per || me >= sh.G) return;
-      done = sh.first(me);
-      shares = sh;
-      left = sh.first(me + 1) - done;
-      if (me > 0) b = paged_locate(p.B, done, work, reinterpret_cast<int*>(smem_raw), index, all);
+      done = shares.first(me);
+      left = shares.first(me + 1) - done;
       b = __builtin_amdgcn_readfirstlane(b);
       index = __builtin_amdgcn_readfirstlane(index);
       const PagedSeq s = paged_seq(p, b);
@@ -102,10 +101,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       items = tile_work(p, s, rb + 1) - tile_work(p, s, rb);
       if (!PREFIX && threadIdx.x == 0) {                          // for the join: how many shares there are, what starts in a block
         const int at = done - item;
-        if (me == 0) p.tile_cuts[0].x = sh.G;
-        else if (item == 0 || sh.group(at) != me - 1) p.tile_cuts[me].y = 0;   // at its start; behind another share's start
+        if (me == 0) p.tile_cuts[0].x = shares.G;
+        else if (item == 0 || shares.group(at) != me - 1) p.tile_cuts[me].y = 0;   // at its start; behind another share's start
         else
-          p.tile_cuts[me] = int4{s.q0 * p.nH + rb * RB, min(s.nq * p.nH - rb * RB, RB), sh.group(at + items - 1), sh.first(me - 1) < at};
+          p.tile_cuts[me] = int4{s.q0 * p.nH + rb * RB, min(s.nq * p.nH - rb * RB, RB), shares.group(at + items - 1), shares.first(me - 1) < at};
       }
     }
     rb = __builtin_amdgcn_readfirstlane(rb);
