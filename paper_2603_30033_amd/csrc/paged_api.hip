@@ -76,6 +76,13 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // (fp32 rows go through paged_rows)
   const int block = tile ? kTileRows : 32;
   a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, tile ? 1 : 2, tile ? 256 : 128) : 0;
+  if (tile && prefix > 0) {
+    // ... and no more of the two workgroups a compute unit than its share of the work, the sequences' own keys at half their bound (128
+    // sequences of up to 2048 rows behind 2048: 33 us, with one workgroup a compute unit for the prefix 39)
+    const double work = (double)prefix * ((rows + block - 1) / block), own = .5 * paged_rows_blocks(a, block) * (keys + kTileBlock * kTileUnit);
+    const long share = (long)(2 * c->n_cus * work / (work + own)) / ((rows + block - 1) / block);
+    a.prefix_parts = (int)std::max(1l, std::min(share, (long)a.prefix_parts));
+  }
   a.prefix_keys = a.prefix_parts > 0 ? part_keys(prefix, a.prefix_parts) : 0;
   const long pieces = (rows + block - 1) / block * a.prefix_parts;
   a.prefix_wgs = (int)((pieces + 7) / 8 * 8);
@@ -97,7 +104,8 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     }
   } else if (tile) {
     const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
-    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31)) a.tile_wgs = std::max(2 * c->n_cus - (int)std::min(pieces, 2l * c->n_cus), c->n_cus);
+    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31))
+      a.tile_wgs = std::max(2 * c->n_cus - (int)std::min(pieces, 2l * c->n_cus), c->n_cus);
     a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
