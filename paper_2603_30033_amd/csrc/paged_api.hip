@@ -93,7 +93,8 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   // behind 16384 rows 44 and 35; 128 with up to 1024 rows of their own 46 and 33; 16 with 32768 68 and 57).
   const int wgs = (stream_late(c->D, f.shared_kv && f.use_rope ? 1 : 0) ? 2 : 1) * c->n_cus;
   const bool split = keys > kStreamWhole;
-  a.hb = !tile || prefix > 0 || (split && (2 * (long)b->B > wgs || b->B > 256)) ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
+  const bool even = 2 * (long)b->B <= wgs && b->B <= 256 && (long)b->B * (keys / kStreamUnit + 1) < (1l << 31);   // (units in 32 bits)
+  a.hb = !tile || prefix > 0 || (split && !even) ? 0 : most <= 32 ? 1 : most <= 64 && c->D < 128 ? 2 : 0;
   a.stream_wgs = a.tile_wgs = 0;
   a.own_parts = prefix > 0 ? 1 : 0;                               // rows that one workgroup does alone
   long shared = 0;                                                // rows of partial results that workgroups share

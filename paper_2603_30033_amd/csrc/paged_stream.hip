@@ -139,11 +139,14 @@ void paged_stream_kernel(PagedArgs p) {
         entry[0] = entry_at(j + 1, 0);
         entry[1] = entry_at(j + 1, 1);
       } else {
-#pragma unroll 1
+        int pages[PIECES];                                       // (all on their way before one is waited for)
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) pages[q] = table[min(divide(min(n0 + q * RPP + l / CPR, keys - 1), p.ps), p.max_pages - 1)];
+#pragma unroll
         for (int q = 0; q < PIECES; ++q) {
           const int row = q * RPP + l / CPR, c = ((l % CPR) ^ swz_x<CPR>(row)) * 8;
-          const int n = min(n0 + row, keys - 1), i = divide(n, p.ps);
-          const long pg = paged_page(table[min(i, p.max_pages - 1)], p.n_pages), a = n - i * p.page_size;
+          const int n = min(n0 + row, keys - 1);
+          const long pg = paged_page(pages[q], p.n_pages), a = n - divide(n, p.ps) * p.page_size;
           const T* kp = static_cast<const T*>(p.K) + pg * p.k_stride + a * p.r3;
           chunk_to_lds(kp + min(c, p.r3 - 8), kt + q * 512);
           if constexpr (KIND == 0) {

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       table = p.table + (long)b * p.max_pages;
       pages = p.max_pages;
     }
-    const int n_rows = nq * p.nH, now = pre ? 1 : min(left, items - item);
+    const int n_rows = nq * p.nH, now = pre ? 1 : max(1, min(left, items - item));
     const bool causal = !pre && p.causal;
     const int r0 = rb * RB, rw = r0 + wave * 32;               // first row of the workgroup, of this wave
     const int r = min(rw + lr, n_rows - 1);                       // rows behind the last repeat it and are not stored
@@ -288,11 +288,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             }
             entry = entry_at(j + 1);
           } else {
-#pragma unroll 1
+            int found[NK];                                        // (all on their way before one is waited for)
+#pragma unroll
+            for (int i = 0; i < NK; ++i) found[i] = table[min(divide(min(n0 + i * RPP + l / CPR, hi_all - 1), p.ps), pages - 1)];
+#pragma unroll
             for (int i = 0; i < NK; ++i) {
               const uint32_t row = i * RPP + l / CPR, c = (l % CPR) ^ swz_x<CPR>(row);
-              const int n = min(n0 + (int)row, hi_all - 1), in_table = divide(n, p.ps);
-              const uint32_t page = paged_page(table[min(in_table, pages - 1)], p.n_pages), at = n - in_table * p.page_size;
+              const int n = min(n0 + (int)row, hi_all - 1);
+              const uint32_t page = paged_page(found[i], p.n_pages), at = n - divide(n, p.ps) * p.page_size;
               chunk_to_lds(static_cast<const u32x4*>(p.K) + (page * k16 + at * rk + min(c, rk - 1)), kt + i * 512);
               if constexpr (KIND == 0)
                 chunk_to_lds(static_cast<const u32x4*>(p.V) + (page * v16 + at * rv + min(c, rv - 1)), kt + L::kTile + i * 512);
@@ -413,8 +416,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     PagedSeq s = paged_seq(p, b);
     if (++rb == tile_blocks(p, s)) {
       rb = 0;
-      do s = paged_seq(p, ++b);
-      while (s.nq == 0);                                          // (work is left, so a sequence with some follows)
+      do {
+        if (++b >= p.B) return;                                   // (work is left, so a sequence follows if q_start never decreases)
+        s = paged_seq(p, b);
+      } while (s.nq == 0);
     }
     items = __builtin_amdgcn_readfirstlane(tile_work(p, s, rb + 1) - tile_work(p, s, rb));
     __syncthreads();
@@ -453,7 +458,7 @@ __global__ __launch_bounds__(256) void paged_tile_join_kernel(PagedArgs p, int g
     live = r < e.y;
     row = (long)e.x + r;
     first = (2 * (g - 1) + e.w) * kTileRows + r;
-    more = e.z - (g - 1);
+    more = max(min(e.z, p.tile_wgs - 1) - (g - 1), 0);
   }
   RowSum sum;
   if (PREFIX ? row < rows : live) {

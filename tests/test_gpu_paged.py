@@ -362,6 +362,23 @@ def test_numbers_that_are_no_page_read_page_0():
         assert torch.isfinite(O[1].float()).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("starts,lens", [([0, 40, 10, 50, 50], [700, 400, 900, 33]), ([-5, 20, 90, 2 ** 31 - 1, 0], [-3, 5000, 800, 2 ** 31 - 1]),
+                                         ([30, 20, 10, 0, -1], [600] * 4)])
+def test_ranges_and_lengths_that_break_the_rules_end_inside_the_buffers(starts, lens, prefix, dtype):
+    # a caller's mistake: results mean nothing, but the call ends, the pool stays as it is and a good call behind it is right
+    b = Batch([40, 0, 9, 1], [700, 400, 900, 333], 16, 64, 64, 12, DT[dtype], prefix=prefix, seed=21)
+    with Context(12, 64, 64, dtype) as c:
+        pages, good = on_gpu(b)
+        before = [t.clone() for t in pages.tensors if t is not None]
+        bad = ta.tucker_attn_batch.of(torch.tensor(starts, dtype=torch.int32).cuda(), torch.tensor(lens, dtype=torch.int32).cuda(),
+                                      torch.where(b.table < len(b.K), b.table, 0).cuda(), tokens=b.T, max_new=40, max_len=900)
+        attend(c, b, pages, bad)
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(before, [t for t in pages.tensors if t is not None]))
+        check(c, b, *attend(c, b, pages, good))
+
+
 # ---- append ----------------------------------------------------------------------------------------------------------
 
 def appended(c, b: Batch, K, V, Q, rotate=True, inplace=False, **kw):
