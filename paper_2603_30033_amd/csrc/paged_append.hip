@@ -68,7 +68,8 @@ template <typename T> __device__ __forceinline__ void turn(Row16<T>& r, const f3
   }
 }
 
-// WIDE: every row starts on 16 bytes.  PAST: rotated queries go past the caches.  parts: groups that a token's rows are dealt to, the last of them its key and value row
+// WIDE: every row starts on 16 bytes.  PAST: rotated queries go past the caches.  parts: groups that a token's rows are dealt to, the
+// last of them its key and value row
 template <typename T, bool WIDE, bool PAST>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, int lanes, int parts) {
   constexpr int N = Row16<T>::N;
@@ -156,7 +157,8 @@ template <typename T> static hipError_t append_one(const PagedAppendArgs& a, hip
   if (blocks > 0x7fffffffl) return hipErrorInvalidValue;
   auto wide = [&](const void* q, long ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * (long)sizeof(T) % 16 == 0; };
   const bool all = wide(a.Kin, a.ldk) && wide(a.Vin, a.ldv) && wide(a.Qin, a.q_row) && wide(a.Qout, a.q_row);
-  const auto kern = !all ? paged_append_kernel<T, false, false> : past ? paged_append_kernel<T, true, true> : paged_append_kernel<T, true, false>;
+  const auto kern = !all ? paged_append_kernel<T, false, false>
+                    : past ? paged_append_kernel<T, true, true> : paged_append_kernel<T, true, false>;
   hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a, lanes, parts);
   return hipGetLastError();
 }

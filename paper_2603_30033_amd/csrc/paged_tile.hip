@@ -77,7 +77,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   } else {
     int index, all;
     if (p.tile_wgs == 0) {                                        // a workgroup for every row block
-      b = paged_locate(p.B, [=](int) { return wg; }, [&](int i) { return tile_blocks(p, paged_seq(p, i)); }, reinterpret_cast<int*>(smem_raw), rb, all);
+      b = paged_locate(p.B, [=](int) { return wg; }, [&](int i) { return tile_blocks(p, paged_seq(p, i)); },
+                       reinterpret_cast<int*>(smem_raw), rb, all);
       if (b < 0) return;
     } else {
       auto start = [&](int total) {                               // of this workgroup's share; behind all if it has none
@@ -133,7 +134,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int r0 = rb * RB, rw = r0 + wave * 32;               // first row of the workgroup, of this wave
     const int r = min(rw + lr, n_rows - 1);                       // rows behind the last repeat it and are not stored
     auto sees = [&](int row) { return causal ? len - nq + divide(min(row, n_rows - 1), p.heads) + 1 : len; };
-    const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);   // keys that the row sees, that all and any rows of the workgroup see
+    // keys that the row sees, that all and any rows of the workgroup see
+    const int limit = sees(r), lo_all = sees(r0), hi_all = sees(r0 + RB - 1);
     const int hi = sees(rw + 31);                                 // keys that any row of the wave sees
     // items dealt to whole units of the keys that the block sees; who ends here and who goes on from here count alike
     const int units = max(0, hi_all - first + kTileUnit - 1) / kTileUnit;
