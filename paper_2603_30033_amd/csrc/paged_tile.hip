@@ -488,7 +488,7 @@ template <int D, int KIND, bool PREFIX> static hipError_t tile_one(const PagedAr
   auto kern = paged_tile_kernel<D, KIND, PREFIX>;
   static LdsOnce lds_once;                                       // one per kernel instantiation
   if (hipError_t e = allow_dynamic_lds(lds_once, kern, smem); e != hipSuccess) return e;
-  const uint32_t own = a.tile_wgs == 0 ? paged_rows_blocks(a, kTileRows) : (uint32_t)((a.tile_wgs + 7) / 8 * 8), grid = own + (PREFIX ? a.prefix_wgs : 0);
+  const uint32_t own = a.tile_wgs == 0 ? paged_rows_blocks(a, kTileRows) : (a.tile_wgs + 7) / 8 * 8, grid = own + (PREFIX ? a.prefix_wgs : 0);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), smem, s, a);
   return hipGetLastError();
 }
