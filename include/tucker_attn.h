@@ -313,6 +313,7 @@ size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tuck
  *   Q    device [T, n_heads, r3]   in: per-head queries, rotated (Qrot of tucker_attn_append_paged)
  *   O    device [T, n_heads, rt3]  out, storage type
  *   lse  device [T, n_heads] fp32  out, natural logarithm; may be NULL
+ *   workspace  device, >= tucker_attn_attend_workspace_bytes bytes (may be NULL if that is 0), 256-byte aligned; scratch
  * One new token per sequence (decode), a few (proposed tokens) or many (pieces of a prompt).  Q and O start on 16 bytes.
  * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more.
  */
@@ -340,6 +341,7 @@ int tucker_attn_attend_prefix(tucker_attn_ctx *ctx, const tucker_attn_pages *pag
  * Serves prompts, pieces of prompts, proposed and single tokens, any mixture of them in one step.  prefix_table may be NULL with
  * prefix_len 0; the prefix's rows are appended beforehand, by a call without one.  Differs from forward and decode in that the
  * per-head queries and outputs pass through memory in the storage type (bf16: two more roundings).
+ *   workspace  device, >= tucker_attn_forward_paged_workspace_bytes bytes, 256-byte aligned; scratch
  * Limits and refusals: those of append and attend above, and 65535 * 32 tokens.
  */
 size_t tucker_attn_forward_paged_workspace_bytes(const tucker_attn_ctx *ctx, const tucker_attn_batch *batch, int32_t prefix_len);
