@@ -105,8 +105,11 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     }
   } else if (tile) {
     const long blocks = paged_rows_blocks(a, block), units = (keys + kTileUnit - 1) / kTileUnit;
-    if (units > kTileLeast && blocks * (units + kTileBlock) < (1l << 31))
-      a.tile_wgs = std::max(2 * c->n_cus - std::min(a.prefix_wgs, 2 * c->n_cus), c->n_cus);   // (every die's workgroups have a place at once)
+    if (const long work = blocks * (units + kTileBlock); units > kTileLeast && work < (1l << 31)) {
+      // every die's workgroups have a place at once beside the prefix's; no more than there can be shares
+      a.tile_wgs = std::max(2 * c->n_cus - std::min(a.prefix_wgs, 2 * c->n_cus), c->n_cus);
+      a.tile_wgs = (int)std::min((long)a.tile_wgs, (work + kTileLeast - 1) / kTileLeast);
+    }
     a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
