@@ -177,7 +177,9 @@ struct RowSum {
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   __device__ __forceinline__ void add(float2 ml, f32x4 v, bool live = true) {
-    live = live && ml.x != -INFINITY;                             // (an empty part's output may never have been written)
+    // An empty part has a sum of 0, and its output may never have been written.  Its maximum says nothing: that of NaN scores alone is
+    // -infinity too, and their sum and output are NaN.
+    live = live && ml.y != 0.f;
     const float top = fmaxf(m, live ? ml.x : -INFINITY), ref = top == -INFINITY ? 0.f : top;
     const float a = fast_exp2(m - ref), f = live ? fast_exp2(ml.x - ref) : 0.f;
     m = top;
