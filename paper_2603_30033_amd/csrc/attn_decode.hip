@@ -757,16 +757,16 @@ __global__ __launch_bounds__(256) void decode_merge_heads_kernel(DecodeArgs p) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (s0 + u * S < p.nsplit) mb = fmaxf(mb, mv[u]);
-        if (mb == -INFINITY) continue;                            // only empty splits so far
-        const float a = fast_exp2(mrun - mb);                     // 0 while mrun is still -inf
+        // -infinity: only splits without a key so far, which add zeros, or of NaN scores, whose sums and outputs are NaN and stay
+        const float ref = mb == -INFINITY ? 0.f : mb;
+        const float a = fast_exp2(mrun - ref);                    // 0 while mrun is still -inf
         den *= a;
 #pragma unroll
         for (int e = 0; e < CPT; ++e) num[e] *= a;
         mrun = mb;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const bool live = s0 + u * S < p.nsplit && mv[u] != -INFINITY;
-          const float w = live ? fast_exp2(mv[u] - mb) : 0.f;
+          const float w = s0 + u * S < p.nsplit ? fast_exp2(mv[u] - ref) : 0.f;
           den += w * lv[u];
 #pragma unroll
           for (int q = 0; q < CPT / 4; ++q)
@@ -786,7 +786,7 @@ __global__ __launch_bounds__(256) void decode_merge_heads_kernel(DecodeArgs p) {
         // reference = the largest of the groups' references; then the parts are scaled and added in group order
         float mall = mrun;
         for (int j = 1; j < S; ++j) mall = fmaxf(mall, px[((tok + j * Bp) * 8 + cg) * (CPT + 2) + CPT]);
-        const float a0 = mrun == -INFINITY ? 0.f : fast_exp2(mrun - mall);   // (mall is finite: some split is not empty)
+        const float a0 = mrun == -INFINITY ? 0.f : fast_exp2(mrun - mall);   // (0 * NaN: NaN)
         den *= a0;
 #pragma unroll
         for (int e = 0; e < CPT; ++e) num[e] *= a0;
