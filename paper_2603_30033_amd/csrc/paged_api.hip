@@ -42,6 +42,10 @@ int check_pool(const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucke
   return TUCKER_ATTN_OK;
 }
 
+// Most new tokens of a sequence: the caller's bound, which may be any number, cut to the tokens there are (so that rows of a sequence are
+// counted in 31 bits like those of the call)
+int most_new(const tucker_attn_batch* b) { return std::min(b->max_new, b->T); }
+
 template <typename A> void fill(A& a, const tucker_attn_ctx* c, const tucker_attn_pages* p, const tucker_attn_batch* b) {
   const tucker_attn_config& f = c->cfg;
   a.K = p->K; a.V = p->V;
@@ -49,7 +53,7 @@ template <typename A> void fill(A& a, const tucker_attn_ctx* c, const tucker_att
   a.v_stride = p->v_stride ? p->v_stride : (long)p->page_size * f.rt3;
   a.n_pages = p->n_pages; a.page_size = p->page_size; a.ps = divisor(p->page_size);
   a.q_start = b->q_start; a.kv_len = b->kv_len; a.table = b->page_table;
-  a.B = b->B; a.T = b->T; a.max_pages = b->max_pages; a.max_new = b->max_new; a.max_len = b->max_len;
+  a.B = b->B; a.T = b->T; a.max_pages = b->max_pages; a.max_new = most_new(b); a.max_len = b->max_len;
   a.nH = f.n_heads; a.r3 = f.r3; a.rt3 = f.rt3;
   a.rope = c->rope; a.rope_ld = f.max_positions;
 }
@@ -71,7 +75,7 @@ constexpr int kStreamWhole = 512;
 size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, void* ws, PagedArgs& a) {
   const tucker_attn_config& f = c->cfg;
   a.B = b->B; a.T = b->T; a.nH = f.n_heads; a.D = c->D; a.prefix = prefix;
-  const long rows = (long)b->T * f.n_heads, most = (long)b->max_new * f.n_heads;
+  const long rows = (long)b->T * f.n_heads, most = (long)most_new(b) * f.n_heads;
   const int keys = b->max_len - prefix;
   const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // (fp32 rows go through paged_rows)
   const int block = tile ? kTileRows : 32;
