@@ -278,8 +278,9 @@ typedef struct {
   const int32_t *page_table;  /* device [B][max_pages]   entries behind a sequence's last page are not looked at          */
   int32_t B, T;
   int32_t max_pages;          /* entries of a table row                                                                   */
-  int32_t max_new, max_len;   /* no sequence brings more new tokens, or has more cached rows; max_len <= max_pages *      */
-                              /* page_size, and <= max_positions with latent RoPE                                         */
+  int32_t max_new, max_len;   /* no sequence brings more new tokens (any number: T of them at most count), or has more    */
+                              /* cached rows; max_len <= max_pages * page_size, and <= max_positions with latent RoPE;    */
+                              /* beyond 2^31 - 2^17 the calls return UNSUPPORTED_SHAPE                                    */
 } tucker_attn_batch;
 
 /*
@@ -293,7 +294,8 @@ typedef struct {
  *            already), and Q must be NULL.  Without latent RoPE nothing is rotated
  * A token before its sequence's first row (kv_len too small) is not stored.  Two tokens that name the same row are a race.
  * Any alignment of K, V, Q, Qrot and of ldk, ldv; rows that start on 16 bytes are read and written whole.
- * UNSUPPORTED_SHAPE: pool rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more.
+ * UNSUPPORTED_SHAPE: pool rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more, or
+ * as many tokens as a launch of 2^24 - 1 workgroups cannot take (T * (1 + n_heads / 8) of about 2^28 with 256-byte rows).
  */
 int tucker_attn_append_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
                              const void *K, int64_t ldk, const void *V, int64_t ldv, const void *Q, void *Qrot,
@@ -315,7 +317,9 @@ size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tuck
  *   lse  device [T, n_heads] fp32  out, natural logarithm; may be NULL
  *   workspace  device, >= tucker_attn_attend_workspace_bytes bytes (may be NULL if that is 0), 256-byte aligned; scratch
  * One new token per sequence (decode), a few (proposed tokens) or many (pieces of a prompt).  Q and O start on 16 bytes.
- * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; a pool of 64 GiB and more; T * n_heads of 2^31 and more.
+ * UNSUPPORTED_SHAPE: rows that are no multiple of 16 bytes; a pool of 64 GiB and more; more than 2^24 - 1 workgroups in a launch:
+ * T * n_heads above 2^31 - 2^8 (fp32: 2^29 - 2^6) with one sequence, 128 (32) less for every other one; behind a prefix above
+ * 2^27 - 8, 2^28 - 16 or 2^29 - 32 with r3 or rt3 above 64, above 32, or neither.
  */
 int tucker_attn_attend_paged(tucker_attn_ctx *ctx, const tucker_attn_pages *pages, const tucker_attn_batch *batch,
                              const void *Q, void *O, float *lse, void *workspace, size_t workspace_bytes,

@@ -81,7 +81,9 @@ struct PagedAppendArgs {
   int rope_ld;
 };
 
+constexpr long kMaxGroups = (1l << 24) - 1;            // workgroups of 256 that a launch takes along x (2^32 threads are refused)
 int paged_rows_blocks(const PagedArgs& a, int rows);   // row blocks of `rows` rows that a batch can have
+bool paged_append_fits(int dtype, const PagedAppendArgs& a);   // into one launch
 hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s);
 hipError_t launch_paged_rows(const PagedArgs& a, bool prefix_pass, hipStream_t s);   // fp32
 hipError_t launch_paged_stream(const PagedArgs& a, hipStream_t s);   // bf16

@@ -15,6 +15,7 @@ hipError_t begin(Recorder& rec) {
 }
 
 constexpr long kMaxRows = 1l << 31;   // (token, head) rows of a call
+constexpr int kMaxLen = (int)((1l << 31) - (1l << 17));   // cached rows of a sequence: the kernels round row numbers up, to whole units and parts
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -22,7 +23,7 @@ int check_batch(const tucker_attn_ctx* c, const tucker_attn_batch* b) {
   if (!c || !b || b->B < 1 || b->T < 1 || b->max_pages < 1 || b->max_new < 1 || b->max_len < 1) return TUCKER_ATTN_INVALID_ARG;
   const tucker_attn_config& f = c->cfg;
   if (f.use_rope && b->max_len > f.max_positions) return TUCKER_ATTN_INVALID_ARG;
-  if ((long)b->T * f.n_heads >= kMaxRows) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
+  if ((long)b->T * f.n_heads >= kMaxRows || b->max_len > kMaxLen) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   if ((f.r3 * c->es) % 16 != 0 || (f.rt3 * c->es) % 16 != 0) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   return TUCKER_ATTN_OK;
 }
@@ -133,6 +134,15 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   return cv.off;
 }
 
+// Whether the launches of a planned call can be made: none has more workgroups than one takes.  (So rows counted in whole blocks stay
+// within 31 bits too.)  Joins that go row by row: D/4 threads each where there are so many rows.
+bool fits(const PagedArgs& a, bool bf16) {
+  const long rows = (long)a.T * a.nH, blocks = paged_rows_blocks(a, bf16 ? kTileRows : 32);
+  if (a.hb > 0) return a.B <= kMaxGroups;
+  if (blocks + (bf16 ? a.prefix_wgs : 0) > kMaxGroups) return false;
+  return a.prefix_parts + a.own_parts == 0 || (rows * (a.D / 4) + 255) / 256 <= kMaxGroups;
+}
+
 int check_prefix(const tucker_attn_batch* b, const int32_t* table, int32_t prefix) {
   return prefix < 0 || prefix > b->max_len || (prefix > 0 && !table) ? TUCKER_ATTN_INVALID_ARG : TUCKER_ATTN_OK;
 }
@@ -176,6 +186,7 @@ int attend(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return TUCKER_ATTN_INVALID_ARG;
   PagedArgs a;
   const size_t need = attend_args(a, c, pages, batch, prefix_table, prefix, workspace);
+  if (!fits(a, c->cfg.dtype == TUCKER_ATTN_BF16)) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   a.Q = Q; a.O = O; a.lse = lse;
   if (need > 0 && !workspace) return TUCKER_ATTN_INVALID_ARG;
   if (workspace_bytes < need) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
@@ -230,6 +241,7 @@ int tucker_attn_append_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages,
   fill(a, c, pages, batch);
   a.Kin = K; a.ldk = ldk; a.Vin = V; a.ldv = ldv; a.Qin = Q; a.Qout = Qrot; a.q_row = f.r3;
   a.rotate_k = rotate && !f.shared_kv;
+  if (!paged_append_fits(f.dtype, a)) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   Recorder rec{c, s, c->profile != 0};
   if (begin(rec) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
@@ -241,7 +253,8 @@ int tucker_attn_append_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages,
 size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx* c, const tucker_attn_batch* batch, int32_t prefix_len) {
   if (check_batch(c, batch) != TUCKER_ATTN_OK || prefix_len < 0 || prefix_len > batch->max_len) return 0;
   PagedArgs a;
-  return plan(c, batch, prefix_len, nullptr, a);
+  const size_t bytes = plan(c, batch, prefix_len, nullptr, a);
+  return fits(a, c->cfg.dtype == TUCKER_ATTN_BF16) ? bytes : 0;
 }
 
 int tucker_attn_attend_paged(tucker_attn_ctx* c, const tucker_attn_pages* pages, const tucker_attn_batch* batch, const void* Q,
@@ -258,7 +271,8 @@ int tucker_attn_attend_prefix(tucker_attn_ctx* c, const tucker_attn_pages* pages
 size_t tucker_attn_forward_paged_workspace_bytes(const tucker_attn_ctx* c, const tucker_attn_batch* batch, int32_t prefix_len) {
   if (check_batch(c, batch) != TUCKER_ATTN_OK || prefix_len < 0 || prefix_len > batch->max_len || batch->T > kMaxTokens) return 0;
   PagedArgs a;
-  return carve_layer(c, nullptr, batch->T).bytes + plan(c, batch, prefix_len, nullptr, a);
+  const size_t bytes = plan(c, batch, prefix_len, nullptr, a);
+  return fits(a, c->cfg.dtype == TUCKER_ATTN_BF16) ? carve_layer(c, nullptr, batch->T).bytes + bytes : 0;
 }
 
 int tucker_attn_forward_paged(tucker_attn_ctx* c, const tucker_attn_weights* w, const void* X, void* Y, const tucker_attn_pages* pages,
@@ -276,6 +290,13 @@ int tucker_attn_forward_paged(tucker_attn_ctx* c, const tucker_attn_weights* w, 
   LayerWs ws = carve_layer(c, workspace, T);
   PagedArgs a;
   const size_t attend_bytes = attend_args(a, c, pages, batch, prefix_table, prefix_len, static_cast<char*>(workspace) + ws.bytes);
+  PagedAppendArgs p;
+  std::memset(&p, 0, sizeof(p));
+  fill(p, c, pages, batch);
+  p.Kin = ws.K; p.ldk = f.r3; p.Vin = f.shared_kv ? nullptr : ws.V; p.ldv = f.rt3;
+  p.Qin = p.Qout = f.use_rope ? ws.Q : nullptr; p.q_row = c->D;   // (queries in place)
+  p.rotate_k = !f.shared_kv;
+  if (!fits(a, f.dtype == TUCKER_ATTN_BF16) || !paged_append_fits(f.dtype, p)) return TUCKER_ATTN_UNSUPPORTED_SHAPE;
   if (workspace_bytes < ws.bytes + attend_bytes) return TUCKER_ATTN_WORKSPACE_TOO_SMALL;
 
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -316,12 +337,6 @@ int tucker_attn_forward_paged(tucker_attn_ctx* c, const tucker_attn_weights* w, 
   if (launch_gemm(f.dtype, q, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("head_queries");
 
-  PagedAppendArgs p;
-  std::memset(&p, 0, sizeof(p));
-  fill(p, c, pages, batch);
-  p.Kin = ws.K; p.ldk = f.r3; p.Vin = f.shared_kv ? nullptr : ws.V; p.ldv = f.rt3;
-  p.Qin = p.Qout = f.use_rope ? ws.Q : nullptr; p.q_row = c->D;   // (queries in place)
-  p.rotate_k = !f.shared_kv;
   if (launch_paged_append(f.dtype, p, s) != hipSuccess) return TUCKER_ATTN_HIP_ERROR;
   (void)rec.after("paged_append");
 

@@ -146,20 +146,30 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs p, in
   if (p.V != nullptr && c < p.rt3) store16<T, true>(static_cast<T*>(p.V) + page * p.v_stride + (long)at * p.rt3 + c, r[1]);
 }
 
+// lanes of a group (a power of two), groups of a token, workgroups
+struct AppendGrid {
+  int lanes = 1, parts;
+  long blocks;
+};
+static AppendGrid append_grid(int es, const PagedAppendArgs& a) {
+  AppendGrid g;
+  const int widest = a.V != nullptr && a.rt3 > a.r3 ? a.rt3 : a.r3;
+  while (g.lanes * 16 < widest * es) g.lanes *= 2;
+  g.parts = 1 + (a.Qin != nullptr ? (a.nH + kAppendHeads - 1) / kAppendHeads : 0);
+  const long slots = 256 / g.lanes;
+  g.blocks = ((long)a.T * g.parts + slots - 1) / slots;
+  return g;
+}
+bool paged_append_fits(int dtype, const PagedAppendArgs& a) { return append_grid(dtype == 0 ? 4 : 2, a).blocks <= kMaxGroups; }
+
 template <typename T> static hipError_t append_one(const PagedAppendArgs& a, hipStream_t s) {
   const bool past = a.Qout != a.Qin && (long)a.T * a.nH * a.q_row * (long)sizeof(T) > kL2Bytes;
-  constexpr int N = Row16<T>::N;
-  const int widest = a.V != nullptr && a.rt3 > a.r3 ? a.rt3 : a.r3;
-  int lanes = 1;                                                  // of a group: a power of two
-  while (lanes * N < widest) lanes *= 2;
-  const int parts = 1 + (a.Qin != nullptr ? (a.nH + kAppendHeads - 1) / kAppendHeads : 0);
-  const long items = (long)a.T * parts, slots = 256 / lanes, blocks = (items + slots - 1) / slots;
-  if (blocks > 0x7fffffffl) return hipErrorInvalidValue;
+  const AppendGrid g = append_grid(sizeof(T), a);
   auto wide = [&](const void* q, long ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * (long)sizeof(T) % 16 == 0; };
   const bool all = wide(a.Kin, a.ldk) && wide(a.Vin, a.ldv) && wide(a.Qin, a.q_row) && wide(a.Qout, a.q_row);
   const auto kern = !all ? paged_append_kernel<T, false, false>
                     : past ? paged_append_kernel<T, true, true> : paged_append_kernel<T, true, false>;
-  hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, s, a, lanes, parts);
+  hipLaunchKernelGGL(kern, dim3((uint32_t)g.blocks), dim3(256), 0, s, a, g.lanes, g.parts);
   return hipGetLastError();
 }
 hipError_t launch_paged_append(int dtype, const PagedAppendArgs& a, hipStream_t s) {
