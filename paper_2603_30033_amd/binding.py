@@ -71,7 +71,11 @@ class tucker_attn_pages(C.Structure):
                 raise TuckerAttnError("a pool is [pages, rows of a page, r] with contiguous pages")
         if V is not None and (V.shape[:2] != K.shape[:2] or V.dtype != K.dtype or V.device != K.device):
             raise TuckerAttnError("key and value pools have the same pages, storage type and device")
-        s = cls(K.data_ptr(), _ptr(V), K.stride(0), 0 if V is None else V.stride(0), K.shape[0], K.shape[1])
+        # (0 says that pages lie one behind the other: an expanded tensor, whose stride that is, would be read behind its end)
+        if K.shape[0] > 1 and any(t is not None and t.stride(0) < t.shape[1] * t.shape[2] for t in (K, V)):
+            raise TuckerAttnError("pages of a pool lie apart: no expanded or overlapping tensor")
+        strides = [0 if t is None or t.shape[0] == 1 else t.stride(0) for t in (K, V)]
+        s = cls(K.data_ptr(), _ptr(V), *strides, K.shape[0], K.shape[1])
         s.tensors = (K, V)
         s.r3, s.rt3, s.dtype = K.shape[2], K.shape[2] if V is None else V.shape[2], K.dtype
         return s
