@@ -78,6 +78,7 @@ class tucker_attn_pages(C.Structure):
         s = cls(K.data_ptr(), _ptr(V), *strides, K.shape[0], K.shape[1])
         s.tensors = (K, V)
         s.r3, s.rt3, s.dtype = K.shape[2], K.shape[2] if V is None else V.shape[2], K.dtype
+        s.kind = (s.r3, s.rt3, {"torch.float32": "f32", "torch.bfloat16": "bf16"}.get(str(K.dtype)))
         return s
 
 
@@ -115,6 +116,8 @@ class tucker_convert_hosvd_info(C.Structure):
 
 
 _lib = None
+# what the calls over pages hold their arrays against, by context handle: heads, model width, (r3, rt3, storage type)
+_contexts: Dict[int, Tuple[int, int, Tuple[int, int, str]]] = {}
 
 
 def load_library() -> C.CDLL:
@@ -234,10 +237,12 @@ def tucker_attn_create(*, d_model, n_heads, d_head, r1, r2, r3, rt1=None, rt2=No
                              int(bool(shared_kv)), int(bool(save_for_backward)))
     ctx = C.c_void_p()
     _check(load_library().tucker_attn_create(C.byref(cfg), C.byref(ctx)), "tucker_attn_create")
+    _contexts[ctx.value] = (cfg.n_heads, cfg.d_model, (cfg.r3, cfg.rt3, dtype))
     return ctx.value
 
 
 def tucker_attn_destroy(ctx: int) -> None:
+    _contexts.pop(ctx, None)
     load_library().tucker_attn_destroy(ctx)
 
 
@@ -354,49 +359,67 @@ def tucker_attn_release_weights(ctx: int) -> None:
 
 # ---- paged latent cache ---------------------------------------------------------------------------------------
 
-def _rows(t, batch: tucker_attn_batch, width: int, pages: tucker_attn_pages, name: str) -> None:
-    if t.shape[0] != batch.T or t.shape[-1] != width or t.dtype != pages.dtype:
-        raise TuckerAttnError(f"{name}: {tuple(t.shape)} {t.dtype} where {batch.T} token rows of {width} {pages.dtype} are expected")
+def _layer_of(ctx, pages: tucker_attn_pages) -> Tuple[int, int]:
+    """Heads and model width of a context, whose cached rows `pages` hold."""
+    if ctx not in _contexts:
+        raise TuckerAttnError("no context of tucker_attn_create")
+    heads, d_model, kind = _contexts[ctx]
+    if pages.kind != kind:
+        raise TuckerAttnError(f"pages of rows (r3, rt3, storage type) {pages.kind} where the context has {kind}")
+    return heads, d_model
+
+
+def _rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
+    if t.shape != shape or t.dtype != pages.dtype:
+        raise TuckerAttnError(f"{name}: {tuple(t.shape)} {t.dtype} where {shape} {pages.dtype} is expected")
+
+
+def _whole_rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
+    _rows(name, t, shape, pages)
+    if not t.is_contiguous():
+        raise TuckerAttnError(f"{name} is contiguous")
 
 
 def tucker_attn_append_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, K, V=None, Q=None, Qrot=None,
                              rotate: bool = True, stream=None, check: bool = True) -> int:
     """K: [T, r3], V: [T, rt3] (None with a shared latent), rows may lie apart (columns of a wider array); Q, Qrot: contiguous
     [T, n_heads, r3], or neither."""
-    _rows(K, batch, pages.r3, pages, "K")
+    heads, _ = _layer_of(ctx, pages)
+    T = batch.T
+    _rows("K", K, (T, pages.r3), pages)
     if V is not None:
-        _rows(V, batch, pages.rt3, pages, "V")
-    for t in (Q, Qrot):
-        if t is not None:
-            _rows(t, batch, pages.r3, pages, "Q, Qrot")
-            if not t.is_contiguous():
-                raise TuckerAttnError("Q and Qrot are contiguous")
+        _rows("V", V, (T, pages.rt3), pages)
     if K.stride(1) != 1 or (V is not None and V.stride(1) != 1):
         raise TuckerAttnError("the channels of a K or V row are contiguous")
-    st = load_library().tucker_attn_append_paged(ctx, C.byref(pages), C.byref(batch), K.data_ptr(), K.stride(0), _ptr(V),
-                                                 0 if V is None else V.stride(0), _ptr(Q), _ptr(Qrot), int(bool(rotate)),
-                                                 _stream_ptr(stream))
+    for t in (Q, Qrot):
+        if t is not None:
+            _whole_rows("Q, Qrot", t, (T, heads, pages.r3), pages)
+    ldk, ldv = (0 if t is None else t.stride(0) if T > 1 else t.shape[1] for t in (K, V))    # (one row has no distance)
+    st = load_library().tucker_attn_append_paged(ctx, C.byref(pages), C.byref(batch), K.data_ptr(), ldk, _ptr(V), ldv, _ptr(Q),
+                                                 _ptr(Qrot), int(bool(rotate)), _stream_ptr(stream))
     if check:
         _check(st, "tucker_attn_append_paged")
     return st
 
 
 def tucker_attn_attend_workspace_bytes(ctx: int, batch: tucker_attn_batch, prefix_len: int = 0) -> int:
-    return int(load_library().tucker_attn_attend_workspace_bytes(ctx, C.byref(batch), prefix_len))
+    return int(load_library().tucker_attn_attend_workspace_bytes(ctx, C.byref(batch), int(prefix_len)))
 
 
-def _attend_rows(pages, batch, Q, O, lse) -> None:
-    _rows(Q, batch, pages.r3, pages, "Q")
-    _rows(O, batch, pages.rt3, pages, "O")
-    if not (Q.is_contiguous() and O.is_contiguous() and (lse is None or lse.is_contiguous())):
-        raise TuckerAttnError("Q, O and lse are contiguous")
+def _attend_rows(ctx, pages, batch, Q, O, lse) -> None:
+    heads, _ = _layer_of(ctx, pages)
+    T = batch.T
+    _whole_rows("Q", Q, (T, heads, pages.r3), pages)
+    _whole_rows("O", O, (T, heads, pages.rt3), pages)
+    if lse is not None and (lse.shape != (T, heads) or str(lse.dtype) != "torch.float32" or not lse.is_contiguous()):
+        raise TuckerAttnError(f"lse: {tuple(lse.shape)} {lse.dtype} where contiguous ({T}, {heads}) torch.float32 is expected")
 
 
 def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, Q, O, lse=None, workspace=None,
                              stream=None, check: bool = True) -> int:
     """Q: [T, n_heads, r3], O: [T, n_heads, rt3], lse: fp32 [T, n_heads] or None; workspace: device uint8 tensor of at least
     tucker_attn_attend_workspace_bytes bytes."""
-    _attend_rows(pages, batch, Q, O, lse)
+    _attend_rows(ctx, pages, batch, Q, O, lse)
     st = load_library().tucker_attn_attend_paged(ctx, C.byref(pages), C.byref(batch), Q.data_ptr(), O.data_ptr(), _ptr(lse),
                                                  _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                                  _stream_ptr(stream))
@@ -414,7 +437,7 @@ def _prefix(pages, prefix_table, prefix_len) -> None:
 def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, prefix_table, prefix_len: int, Q, O,
                               lse=None, workspace=None, stream=None, check: bool = True) -> int:
     """tucker_attn_attend_paged behind a common prefix; prefix_table: int32 device tensor with the pages of its rows."""
-    _attend_rows(pages, batch, Q, O, lse)
+    _attend_rows(ctx, pages, batch, Q, O, lse)
     _prefix(pages, prefix_table, prefix_len)
     st = load_library().tucker_attn_attend_prefix(ctx, C.byref(pages), C.byref(batch), _ptr(prefix_table), int(prefix_len),
                                                   Q.data_ptr(), O.data_ptr(), _ptr(lse), _ptr(workspace),
@@ -432,9 +455,9 @@ def tucker_attn_forward_paged(ctx: int, weights: Dict, X, Y, pages: tucker_attn_
                               prefix_len: int = 0, workspace=None, stream=None, check: bool = True) -> int:
     """X, Y: contiguous [T, d_model], the tokens of all sequences one sequence behind the other; weights: dict of contiguous device
     tensors; workspace: device uint8 tensor of at least tucker_attn_forward_paged_workspace_bytes bytes."""
-    for t in (X, Y):
-        if t.dim() != 2 or t.shape[0] != batch.T or t.shape != X.shape or t.dtype != pages.dtype or not t.is_contiguous():
-            raise TuckerAttnError(f"X, Y: {tuple(t.shape)} {t.dtype} where {batch.T} contiguous rows of {pages.dtype} are expected")
+    _, d_model = _layer_of(ctx, pages)
+    for name, t in (("X", X), ("Y", Y)):
+        _whole_rows(name, t, (batch.T, d_model), pages)
     _prefix(pages, prefix_table, prefix_len)
     ws = _weights_struct(weights)
     st = load_library().tucker_attn_forward_paged(ctx, C.byref(ws), X.data_ptr(), Y.data_ptr(), C.byref(pages), C.byref(batch),
