@@ -78,6 +78,7 @@ class tucker_attn_pages(C.Structure):
         s = cls(K.data_ptr(), _ptr(V), *strides, K.shape[0], K.shape[1])
         s.tensors = (K, V)
         s.r3, s.rt3, s.dtype = K.shape[2], K.shape[2] if V is None else V.shape[2], K.dtype
+        s.device = K.get_device()                                   # its index; -1: host memory
         s.kind = (s.r3, s.rt3, {"torch.float32": "f32", "torch.bfloat16": "bf16"}.get(str(K.dtype)))
         return s
 
@@ -95,11 +96,11 @@ class tucker_attn_batch(C.Structure):
         if tuple(q_start.shape) != (B + 1,) or page_table.dim() != 2 or page_table.shape[0] != B:
             raise TuckerAttnError("q_start is [B + 1], kv_len [B], page_table [B, max_pages]")
         for t in (q_start, kv_len, page_table):
-            if str(t.dtype) != "torch.int32" or not t.is_contiguous():
-                raise TuckerAttnError("the arrays of a batch are contiguous int32 tensors")
+            if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.device != kv_len.device:
+                raise TuckerAttnError("the arrays of a batch are contiguous int32 tensors on one device")
         s = cls(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), B, int(tokens), int(page_table.shape[1]),
                 int(max_new), int(max_len))
-        s.tensors = (q_start, kv_len, page_table)
+        s.tensors, s.device = (q_start, kv_len, page_table), kv_len.get_device()
         return s
 
 
@@ -374,6 +375,19 @@ def _rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> Non
         raise TuckerAttnError(f"{name}: {tuple(t.shape)} {t.dtype} where {shape} {pages.dtype} is expected")
 
 
+def _paged_stream_ptr(stream, pages: tucker_attn_pages, batch: tucker_attn_batch, *tensors) -> Optional[int]:
+    """The stream's handle, of the GPU that holds the pool and everything else of a call and is the current one."""
+    import torch
+    device = pages.device
+    if device < 0 or batch.device != device or any(t is not None and t.get_device() != device for t in tensors):
+        raise TuckerAttnError("pools, batches, arrays and workspace of a call over pages are on one GPU")
+    if device != torch.cuda.current_device() or (stream is not None and stream.device_index != device):
+        raise TuckerAttnError(f"a pool on GPU {device}: the calls over pages run on the current GPU, on a stream of it")
+    if stream is not None:
+        return stream.cuda_stream or None
+    return torch._C._cuda_getCurrentRawStream(device) or None
+
+
 def _whole_rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
     _rows(name, t, shape, pages)
     if not t.is_contiguous():
@@ -395,8 +409,9 @@ def tucker_attn_append_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_a
         if t is not None:
             _whole_rows("Q, Qrot", t, (T, heads, pages.r3), pages)
     ldk, ldv = (0 if t is None else t.stride(0) if T > 1 else t.shape[1] for t in (K, V))    # (one row has no distance)
+    stream_ptr = _paged_stream_ptr(stream, pages, batch, K, V, Q, Qrot)
     st = load_library().tucker_attn_append_paged(ctx, C.byref(pages), C.byref(batch), K.data_ptr(), ldk, _ptr(V), ldv, _ptr(Q),
-                                                 _ptr(Qrot), int(bool(rotate)), _stream_ptr(stream))
+                                                 _ptr(Qrot), int(bool(rotate)), stream_ptr)
     if check:
         _check(st, "tucker_attn_append_paged")
     return st
@@ -420,9 +435,10 @@ def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_a
     """Q: [T, n_heads, r3], O: [T, n_heads, rt3], lse: fp32 [T, n_heads] or None; workspace: device uint8 tensor of at least
     tucker_attn_attend_workspace_bytes bytes."""
     _attend_rows(ctx, pages, batch, Q, O, lse)
+    stream_ptr = _paged_stream_ptr(stream, pages, batch, Q, O, lse, workspace)
     st = load_library().tucker_attn_attend_paged(ctx, C.byref(pages), C.byref(batch), Q.data_ptr(), O.data_ptr(), _ptr(lse),
                                                  _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                                 _stream_ptr(stream))
+                                                 stream_ptr)
     if check:
         _check(st, "tucker_attn_attend_paged")
     return st
@@ -439,9 +455,10 @@ def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_
     """tucker_attn_attend_paged behind a common prefix; prefix_table: int32 device tensor with the pages of its rows."""
     _attend_rows(ctx, pages, batch, Q, O, lse)
     _prefix(pages, prefix_table, prefix_len)
+    stream_ptr = _paged_stream_ptr(stream, pages, batch, prefix_table, Q, O, lse, workspace)
     st = load_library().tucker_attn_attend_prefix(ctx, C.byref(pages), C.byref(batch), _ptr(prefix_table), int(prefix_len),
                                                   Q.data_ptr(), O.data_ptr(), _ptr(lse), _ptr(workspace),
-                                                  0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+                                                  0 if workspace is None else workspace.numel(), stream_ptr)
     if check:
         _check(st, "tucker_attn_attend_prefix")
     return st
@@ -459,10 +476,11 @@ def tucker_attn_forward_paged(ctx: int, weights: Dict, X, Y, pages: tucker_attn_
     for name, t in (("X", X), ("Y", Y)):
         _whole_rows(name, t, (batch.T, d_model), pages)
     _prefix(pages, prefix_table, prefix_len)
+    stream_ptr = _paged_stream_ptr(stream, pages, batch, *weights.values(), X, Y, prefix_table, workspace)
     ws = _weights_struct(weights)
     st = load_library().tucker_attn_forward_paged(ctx, C.byref(ws), X.data_ptr(), Y.data_ptr(), C.byref(pages), C.byref(batch),
                                                   _ptr(prefix_table), int(prefix_len), _ptr(workspace),
-                                                  0 if workspace is None else workspace.numel(), _stream_ptr(stream))
+                                                  0 if workspace is None else workspace.numel(), stream_ptr)
     if check:
         _check(st, "tucker_attn_forward_paged")
     return st

@@ -84,3 +84,31 @@ def test_handles_that_are_no_context(pages, call):
     for bad in (c, None, 0):
         with pytest.raises(ta.TuckerAttnError, match="no context"):
             CALLS[call](bad, pages, batch(), GOOD)
+
+
+@pytest.mark.parametrize("call", sorted(CALLS))
+def test_host_memory(ctx, pages, call):
+    with pytest.raises(ta.TuckerAttnError, match="one GPU"):
+        CALLS[call](ctx, pages, batch(), GOOD)
+
+
+def test_batches_on_two_devices():
+    i32 = lambda *s, **kw: torch.zeros(*s, dtype=torch.int32, **kw)
+    with pytest.raises(ta.TuckerAttnError, match="one device"):
+        ta.tucker_attn_batch.of(i32(3), i32(2, device="meta"), i32(2, 4), tokens=2, max_new=1, max_len=64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("call,names", [("append", ["K", "V", "Q", "Qrot"]), ("attend", ["Q", "O", "lse", "workspace"]),
+                                        ("prefix", ["Q", "O", "lse", "workspace", "prefix_table"]), ("layer", ["X", "Y", "workspace", "prefix_table"])])
+def test_arrays_in_host_memory_beside_a_pool_on_the_gpu(ctx, call, names):
+    good = dict({k: None if v is None else v.cuda() for k, v in GOOD.items()}, lse=torch.zeros(2, 4, device="cuda"))
+    pool = ta.tucker_attn_pages.of(zeros(4, 16, 32).cuda(), zeros(4, 16, 64).cuda())
+    for name in names:
+        with pytest.raises(ta.TuckerAttnError, match="one GPU"):
+            CALLS[call](ctx, pool, batch(device="cuda"), dict(good, **{name: good[name].cpu()}))
+    with pytest.raises(ta.TuckerAttnError, match="one GPU"):
+        CALLS[call](ctx, pool, batch(), good)
+    if call == "layer":
+        with pytest.raises(ta.TuckerAttnError, match="one GPU"):
+            ta.tucker_attn_forward_paged(ctx, {"C": zeros(4)}, good["X"], good["Y"], pool, batch(device="cuda"), workspace=good["workspace"])
