@@ -370,17 +370,28 @@ def _layer_of(ctx, pages: tucker_attn_pages) -> Tuple[int, int]:
     return heads, d_model
 
 
+_ONE_GPU = "pools, batches, arrays and workspace of a call over pages are on one GPU"
+
+
 def _rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
     if t.shape != shape or t.dtype != pages.dtype:
         raise TuckerAttnError(f"{name}: {tuple(t.shape)} {t.dtype} where {shape} {pages.dtype} is expected")
+    if t.get_device() != pages.device:
+        raise TuckerAttnError(f"{name}: {_ONE_GPU}")
 
 
-def _paged_stream_ptr(stream, pages: tucker_attn_pages, batch: tucker_attn_batch, *tensors) -> Optional[int]:
-    """The stream's handle, of the GPU that holds the pool and everything else of a call and is the current one."""
+def _whole_rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
+    _rows(name, t, shape, pages)
+    if not t.is_contiguous():
+        raise TuckerAttnError(f"{name} is contiguous")
+
+
+def _paged_stream_ptr(stream, pages: tucker_attn_pages, batch: tucker_attn_batch) -> Optional[int]:
+    """The stream's handle, of the GPU that holds pool and batch and is the current one."""
     import torch
     device = pages.device
-    if device < 0 or batch.device != device or any(t is not None and t.get_device() != device for t in tensors):
-        raise TuckerAttnError("pools, batches, arrays and workspace of a call over pages are on one GPU")
+    if device < 0 or batch.device != device:
+        raise TuckerAttnError(_ONE_GPU)
     if device != torch.cuda.current_device() or (stream is not None and stream.device_index != device):
         raise TuckerAttnError(f"a pool on GPU {device}: the calls over pages run on the current GPU, on a stream of it")
     if stream is not None:
@@ -388,10 +399,12 @@ def _paged_stream_ptr(stream, pages: tucker_attn_pages, batch: tucker_attn_batch
     return torch._C._cuda_getCurrentRawStream(device) or None
 
 
-def _whole_rows(name: str, t, shape: Tuple[int, ...], pages: tucker_attn_pages) -> None:
-    _rows(name, t, shape, pages)
-    if not t.is_contiguous():
-        raise TuckerAttnError(f"{name} is contiguous")
+def _paged_workspace(workspace, pages: tucker_attn_pages) -> Tuple[Optional[int], int]:
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != pages.device:
+        raise TuckerAttnError(f"workspace: {_ONE_GPU}")
+    return workspace.data_ptr(), workspace.numel()
 
 
 def tucker_attn_append_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, K, V=None, Q=None, Qrot=None,
@@ -401,17 +414,22 @@ def tucker_attn_append_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_a
     heads, _ = _layer_of(ctx, pages)
     T = batch.T
     _rows("K", K, (T, pages.r3), pages)
+    ldk, channel = K.stride()
+    ldv = 0
     if V is not None:
         _rows("V", V, (T, pages.rt3), pages)
-    if K.stride(1) != 1 or (V is not None and V.stride(1) != 1):
+        ldv, channel_v = V.stride()
+        channel = channel if channel_v == 1 else 0
+    if channel != 1:
         raise TuckerAttnError("the channels of a K or V row are contiguous")
-    for t in (Q, Qrot):
-        if t is not None:
-            _whole_rows("Q, Qrot", t, (T, heads, pages.r3), pages)
-    ldk, ldv = (0 if t is None else t.stride(0) if T > 1 else t.shape[1] for t in (K, V))    # (one row has no distance)
-    stream_ptr = _paged_stream_ptr(stream, pages, batch, K, V, Q, Qrot)
+    if T == 1:                                                      # one row has no distance
+        ldk, ldv = pages.r3, pages.rt3
+    if Q is not None:
+        _whole_rows("Q", Q, (T, heads, pages.r3), pages)
+    if Qrot is not None:
+        _whole_rows("Qrot", Qrot, (T, heads, pages.r3), pages)
     st = load_library().tucker_attn_append_paged(ctx, C.byref(pages), C.byref(batch), K.data_ptr(), ldk, _ptr(V), ldv, _ptr(Q),
-                                                 _ptr(Qrot), int(bool(rotate)), stream_ptr)
+                                                 _ptr(Qrot), int(bool(rotate)), _paged_stream_ptr(stream, pages, batch))
     if check:
         _check(st, "tucker_attn_append_paged")
     return st
@@ -426,8 +444,12 @@ def _attend_rows(ctx, pages, batch, Q, O, lse) -> None:
     T = batch.T
     _whole_rows("Q", Q, (T, heads, pages.r3), pages)
     _whole_rows("O", O, (T, heads, pages.rt3), pages)
-    if lse is not None and (lse.shape != (T, heads) or str(lse.dtype) != "torch.float32" or not lse.is_contiguous()):
+    if lse is None:
+        return
+    if lse.shape != (T, heads) or lse.element_size() != 4 or not lse.is_floating_point() or not lse.is_contiguous():
         raise TuckerAttnError(f"lse: {tuple(lse.shape)} {lse.dtype} where contiguous ({T}, {heads}) torch.float32 is expected")
+    if lse.get_device() != pages.device:
+        raise TuckerAttnError(f"lse: {_ONE_GPU}")
 
 
 def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, Q, O, lse=None, workspace=None,
@@ -435,19 +457,21 @@ def tucker_attn_attend_paged(ctx: int, pages: tucker_attn_pages, batch: tucker_a
     """Q: [T, n_heads, r3], O: [T, n_heads, rt3], lse: fp32 [T, n_heads] or None; workspace: device uint8 tensor of at least
     tucker_attn_attend_workspace_bytes bytes."""
     _attend_rows(ctx, pages, batch, Q, O, lse)
-    stream_ptr = _paged_stream_ptr(stream, pages, batch, Q, O, lse, workspace)
     st = load_library().tucker_attn_attend_paged(ctx, C.byref(pages), C.byref(batch), Q.data_ptr(), O.data_ptr(), _ptr(lse),
-                                                 _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                                 stream_ptr)
+                                                 *_paged_workspace(workspace, pages), _paged_stream_ptr(stream, pages, batch))
     if check:
         _check(st, "tucker_attn_attend_paged")
     return st
 
 
 def _prefix(pages, prefix_table, prefix_len) -> None:
-    if prefix_len > 0 and prefix_table is not None and (str(prefix_table.dtype) != "torch.int32" or not prefix_table.is_contiguous() or
-                                                        prefix_table.numel() * pages.page_size < prefix_len):
+    if prefix_table is None:
+        return
+    if prefix_len > 0 and (str(prefix_table.dtype) != "torch.int32" or not prefix_table.is_contiguous() or
+                           prefix_table.numel() * pages.page_size < prefix_len):
         raise TuckerAttnError("prefix_table: int32, a page for every page_size rows of the prefix")
+    if prefix_table.get_device() != pages.device:
+        raise TuckerAttnError(f"prefix_table: {_ONE_GPU}")
 
 
 def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_attn_batch, prefix_table, prefix_len: int, Q, O,
@@ -455,10 +479,9 @@ def tucker_attn_attend_prefix(ctx: int, pages: tucker_attn_pages, batch: tucker_
     """tucker_attn_attend_paged behind a common prefix; prefix_table: int32 device tensor with the pages of its rows."""
     _attend_rows(ctx, pages, batch, Q, O, lse)
     _prefix(pages, prefix_table, prefix_len)
-    stream_ptr = _paged_stream_ptr(stream, pages, batch, prefix_table, Q, O, lse, workspace)
     st = load_library().tucker_attn_attend_prefix(ctx, C.byref(pages), C.byref(batch), _ptr(prefix_table), int(prefix_len),
-                                                  Q.data_ptr(), O.data_ptr(), _ptr(lse), _ptr(workspace),
-                                                  0 if workspace is None else workspace.numel(), stream_ptr)
+                                                  Q.data_ptr(), O.data_ptr(), _ptr(lse), *_paged_workspace(workspace, pages),
+                                                  _paged_stream_ptr(stream, pages, batch))
     if check:
         _check(st, "tucker_attn_attend_prefix")
     return st
@@ -476,11 +499,12 @@ def tucker_attn_forward_paged(ctx: int, weights: Dict, X, Y, pages: tucker_attn_
     for name, t in (("X", X), ("Y", Y)):
         _whole_rows(name, t, (batch.T, d_model), pages)
     _prefix(pages, prefix_table, prefix_len)
-    stream_ptr = _paged_stream_ptr(stream, pages, batch, *weights.values(), X, Y, prefix_table, workspace)
+    if any(t is not None and t.get_device() != pages.device for t in weights.values()):
+        raise TuckerAttnError(f"weights: {_ONE_GPU}")
     ws = _weights_struct(weights)
     st = load_library().tucker_attn_forward_paged(ctx, C.byref(ws), X.data_ptr(), Y.data_ptr(), C.byref(pages), C.byref(batch),
-                                                  _ptr(prefix_table), int(prefix_len), _ptr(workspace),
-                                                  0 if workspace is None else workspace.numel(), stream_ptr)
+                                                  _ptr(prefix_table), int(prefix_len), *_paged_workspace(workspace, pages),
+                                                  _paged_stream_ptr(stream, pages, batch))
     if check:
         _check(st, "tucker_attn_forward_paged")
     return st
