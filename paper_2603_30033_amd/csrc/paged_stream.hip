@@ -192,6 +192,13 @@ void paged_stream_kernel(PagedArgs p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[hb][e] = 0.f;
       if constexpr (ROT) {
+        // products with the keys' second parts have sums of their own: where a key is infinite, what its first part leaves over is
+        // Inf - Inf, and that score is the first part's alone (a finite number added to it changes nothing)
+        f32x16 sr[HB];
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sr[hb][e] = 0.f;
         const f32x4* rl = reinterpret_cast<const f32x4*>(kt + L::kTile);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -212,9 +219,13 @@ void paged_stream_kernel(PagedArgs p) {
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb) {
             mma32(sc[hb], kf, qf[hb][cb]);
-            mma32(sc[hb], rest, qf[hb][cb]);
+            mma32(sr[hb], rest, qf[hb][cb]);
           }
         }
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sc[hb][e] += __builtin_amdgcn_fmed3f(sr[hb][e], -3.4e38f, 3.4e38f);   // (of a NaN: a bound)
       } else {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {

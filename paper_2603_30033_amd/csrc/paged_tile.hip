@@ -351,15 +351,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             const int ch = ch0 + 8 * i;
             if (ch >= CPR) break;
             u32x4 hi16, lo16;
+            float most = 0.f;
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
               const float c = reg.cs[i][d / 2][2 * (d % 2)], sn = reg.cs[i][d / 2][2 * (d % 2) + 1];
               const float x0 = __uint_as_float(reg.x[i][d] << 16), x1 = __uint_as_float(reg.x[i][d] & 0xffff0000u);
               const f32x2 y = {x0 * c - x1 * sn, x0 * sn + x1 * c};
+              most = fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), most);
               hi16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
               const f32x2 z = {y[0] - __uint_as_float(hi16[d] << 16), y[1] - __uint_as_float(hi16[d] & 0xffff0000u)};
               lo16[d] = __builtin_bit_cast(uint32_t, __builtin_convertvector(z, bf16x2));
             }
+            // the first part of an infinite channel leaves Inf - Inf: nothing of it is kept
+            if (most > 3.38e38f)                                    // (rare)
+#pragma unroll
+              for (int d = 0; d < 4; ++d) {
+                const uint32_t bad = (((hi16[d] & Bits<T>::kExp) + Bits<T>::kLow) >> Bits<T>::kSign) & Bits<T>::kUnit;
+                lo16[d] &= ~(bad * Bits<T>::kAll);
+              }
             const int at = row * D + ((ch ^ swz_x<CPR>(row)) * 8);
             *reinterpret_cast<u32x4*>(kt + at) = hi16;
             *reinterpret_cast<u32x4*>(kt + L::kTile + at) = lo16;

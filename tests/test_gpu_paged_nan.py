@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_reference import Batch
+from paged_reference import Batch, turned
 from paper_2603_30033_amd import workloads as wl
 from paper_2603_30033_amd.device import Layer, to_device, to_host
 from test_gpu_forward_paged import Server, inputs
@@ -80,3 +80,40 @@ def test_a_token_of_the_layer_that_is_nan(prefix, dtype):
             kw = dict(prefix_table=torch.tensor(s.tables[0][:prefix // 16], dtype=torch.int32).cuda(), prefix_len=prefix)
         y = s.step(X, [1, 1], **kw)
     assert np.isnan(y[0]).all() and np.isfinite(y[1]).all()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,heads,r", LAYERS + [("bf16", 4, 32), ("bf16", 40, 96)])
+@pytest.mark.parametrize("call", sorted(CALLS))
+def test_an_infinite_channel_of_a_shared_latent(call, dtype, heads, r, sign):
+    # row 1 turned by one radian: both channels of its first pair become sign * inf, and scores -inf where the query's are -sign.  A key
+    # of weight 0 leaves the log-sum-exp and all channels but its infinite one (0 * inf) as the sums over the other rows have them
+    new, rows, prefix = CALLS[call]
+    b = Batch(new, rows, 16, r, r, heads, DT[dtype], shared=True, prefix=prefix, seed=33, fill=0.0)
+    b.Q[..., :2] = -sign * (b.Q[..., :2].float().abs() + 0.5).to(DT[dtype])
+    at = b.rows_of(0)[1]                                          # of the prefix every sequence's, else of the first sequence
+    b.K.view(-1, r)[at, 0] = -sign * 30.0                         # its weight is large: the sums without it are others
+    far = run(b, heads, r, dtype, True)
+    b.K.view(-1, r)[at, 0] = sign * math.inf
+    O, L = run(b, heads, r, dtype, True)
+    sees = torch.arange(b.T) < (b.T if prefix else new[0])
+    assert torch.isfinite(L).all() and torch.isfinite(O[..., 1:]).all()
+    assert not torch.isfinite(O[sees][..., 0]).any() and torch.isfinite(O[~sees]).all()
+    assert torch.equal(O[~sees], far[0][~sees])
+    with_zero = b.K.view(-1, r)[at].clone()
+    b.K.view(-1, r)[at] = 0.0                                     # the definition: the row taken out
+    K = b.K.double()
+    for t in range(min(int(sees.sum()), 8)):
+        s = next(i for i in range(b.B) if t < int(b.q_start[i + 1]))
+        keep = [i for i in range(rows[s] - new[s] + t - int(b.q_start[s]) + 1) if i != 1]
+        X = K.view(-1, r)[b.rows_of(s)[keep]]
+        S = b.Q[t].double() @ turned(X, torch.tensor(keep), b.base).T / 8.0
+        ref, lse = torch.softmax(S, -1) @ X, torch.logsumexp(S, -1)
+        err = (O[t, :, 1:].cpu().double() - ref[:, 1:]).norm() / ref[:, 1:].norm()
+        assert err <= (4e-3 if dtype == "bf16" else 1e-5)
+        # a rotated key is two bf16 parts (2^-8 of 2^-8 of it is lost) of a turn in fp32, a score an fp32 sum, exponentials 2^-21
+        pairs = (X[:, 0::2].abs() + X[:, 1::2].abs()).repeat_interleave(2, 1)
+        size = (b.Q[t].double().abs() @ pairs.T / 8.0).amax(-1)
+        tol = size * ((2.0 ** -16 if dtype == "bf16" else 0) + (r + 2) * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -21 + (len(keep) + 64) * 2.0 ** -24
+        assert ((L[t].cpu().double() - lse).abs() <= tol + lse.abs() * 2.0 ** -22).all()
+    assert torch.isinf(with_zero[0])
