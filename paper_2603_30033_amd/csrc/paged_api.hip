@@ -59,15 +59,20 @@ template <typename A> void fill(A& a, const tucker_attn_ctx* c, const tucker_att
   a.rope = c->rope; a.rope_ld = f.max_positions;
 }
 
-// Parts that the keys of a product of `blocks` row blocks are dealt to: `wgs` workgroups for every compute unit, and no part of
-// fewer than `least` keys
+// Parts that the keys of a product of `blocks` row blocks are dealt to: `wgs` workgroups for every compute unit, and no more parts than
+// ones of `least` keys would be
 int key_parts(const tucker_attn_ctx* c, long blocks, int keys, int wgs, int least) {
   const long most = (keys + least - 1) / least, want = (long)wgs * c->n_cus / (blocks < 1 ? 1 : blocks);
   return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
-// Keys of each of these parts: whole tiles
-int part_keys(int keys, int parts) { return keys < 1 ? 64 : ((keys + parts - 1) / parts + 63) / 64 * 64; }
+// Keys of each of these parts, whole tiles; and the parts that then hold any (4097 keys in 16 parts: 13 of 320)
+int part_keys(int keys, int& parts) {
+  if (keys < 1) return 64;
+  const int each = ((keys + parts - 1) / parts + 63) / 64 * 64;
+  parts = (keys + each - 1) / each;
+  return each;
+}
 
 // Longest keys that one workgroup takes alone rather than several and a second launch that joins their results
 constexpr int kStreamWhole = 512;
@@ -118,7 +123,7 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
-    const int parts = key_parts(c, paged_rows_blocks(a, block), keys, 2, 128);
+    int parts = key_parts(c, paged_rows_blocks(a, block), keys, 2, 128);
     a.own_keys = part_keys(keys, parts);
     if (parts > 1) a.own_parts = parts;
   }

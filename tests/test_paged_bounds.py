@@ -71,3 +71,18 @@ def test_more_tokens_than_an_append_has_workgroups():
             assert append(T) == -2, T
     finally:
         ta.tucker_attn_destroy(c)
+
+
+@pytest.mark.parametrize("T", [1, 8, 48, 256, 300])
+def test_no_part_of_a_prefix_is_empty(T):
+    # fp32: partial results of the prefix's parts and one of the sequences' own keys, D floats and two more a row
+    c = ta.tucker_attn_create(d_model=64, n_heads=4, d_head=16, r1=1, r2=32, r3=64, rt3=64, dtype="f32", max_positions=8)
+    try:
+        for keys in list(range(100, 1000, 37)) + [4097, 5000, 16384]:
+            b = batch(B=1, T=T, max_new=T, max_pages=2 ** 12, max_len=keys + 64)
+            rows, n = 4 * T, ta.tucker_attn_attend_workspace_bytes(c, b, keys)
+            pad = lambda x: (x + 255) // 256 * 256
+            parts = next(p for p in range(1, 2000) if pad(p * rows * 256) + pad(p * rows * 8) == n) - 1
+            assert any(-(-keys // each) == parts for each in range(64, keys + 64, 64)), (keys, parts)
+    finally:
+        ta.tucker_attn_destroy(c)
