@@ -47,7 +47,7 @@ class Layer:
             self.weights = {k: device_weights[k] for k in W_KEYS if not (w.shared_kv and k == "Ut3")}
         else:
             self.weights = {k: to_device(inp[k], w.dtype) for k in W_KEYS if not (w.shared_kv and k == "Ut3")}
-        self._ws = None
+        self._ws, self._ws_captured, self._ws_of_graphs = None, False, []
 
     def close(self):
         if self.ctx is not None:
@@ -68,7 +68,10 @@ class Layer:
 
     def workspace(self, nbytes: int) -> torch.Tensor:
         if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda")
+            if self._ws_captured:
+                self._ws_of_graphs.append(self._ws)               # replays go on writing there
+            self._ws, self._ws_captured = torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda"), False
+        self._ws_captured = self._ws_captured or torch.cuda.is_current_stream_capturing()
         return self._ws
 
     def forward(self, X: torch.Tensor, pos0: int = 0, Kc=None, Vc=None, Y=None) -> torch.Tensor:
