@@ -98,6 +98,8 @@ class tucker_attn_batch(C.Structure):
         for t in (q_start, kv_len, page_table):
             if str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.device != kv_len.device:
                 raise TuckerAttnError("the arrays of a batch are contiguous int32 tensors on one device")
+        if not all(0 <= v < 2 ** 31 for v in (tokens, max_new, max_len, page_table.shape[1])):
+            raise TuckerAttnError("tokens, max_new, max_len and the pages of a sequence are counted in 31 bits")   # (not cut to their low ones)
         s = cls(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), B, int(tokens), int(page_table.shape[1]),
                 int(max_new), int(max_len))
         s.tensors, s.device = (q_start, kv_len, page_table), kv_len.get_device()

@@ -112,3 +112,10 @@ def test_arrays_in_host_memory_beside_a_pool_on_the_gpu(ctx, call, names):
     if call == "layer":
         with pytest.raises(ta.TuckerAttnError, match="one GPU"):
             ta.tucker_attn_forward_paged(ctx, {"C": zeros(4)}, good["X"], good["Y"], pool, batch(device="cuda"), workspace=good["workspace"])
+
+
+def test_bounds_that_need_more_than_31_bits():
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    for bad in (dict(tokens=2 ** 32 + 2), dict(max_new=2 ** 31), dict(max_new=2 ** 32 + 1), dict(max_len=2 ** 32 + 64), dict(max_len=-1)):
+        with pytest.raises(ta.TuckerAttnError, match="31 bits"):
+            ta.tucker_attn_batch.of(i32(3), i32(2), i32(2, 4), **dict(dict(tokens=2, max_new=1, max_len=64), **bad))
