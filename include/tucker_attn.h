@@ -238,7 +238,8 @@ int tucker_attn_backward(tucker_attn_ctx *ctx, const tucker_attn_weights *w,
  * Weights that stay fixed over many calls (serving): prepare their operand-layout copies once
  * (the head-mixed cores G_i = sum_a U1[i,a] C[a] of Section "KV Caching" and the transposed, padded
  * factor matrices, step one of every forward / decode call) into a caller-owned device buffer, and
- * every later forward / decode / backward call (over pages too) of this context skips that step.
+ * every later forward / decode / backward call (over pages too) of this context skips that step.  (The buffer holds what
+ * each of them needs: the cores twice for the queries, fragment by fragment and in rows for the calls over pages.)
  *   prepared   device, >= tucker_attn_prepared_weights_bytes(ctx) bytes, 256-byte aligned
  * Exception to the ownership rule above: the context keeps the pointer `prepared` and the eight
  * weight pointers of `w` until tucker_attn_release_weights or tucker_attn_destroy; the caller keeps
@@ -273,7 +274,8 @@ typedef struct {
  * page number outside the pool is read as page 0 and not written. */
 typedef struct {
   const int32_t *q_start;     /* device [B+1]            q_start[0] = 0, not decreasing, q_start[B] <= T: the token rows behind */
-                              /*                         it are padding, neither read nor written                        */
+                              /*                         it are padding, whose contents do not matter and whose results  */
+                              /*                         are not written (but rows of Y in the layer's call)             */
   const int32_t *kv_len;      /* device [B]              at least the sequence's number of new tokens                     */
   const int32_t *page_table;  /* device [B][max_pages]   entries behind a sequence's last page are not looked at          */
   int32_t B, T;
@@ -311,7 +313,11 @@ size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tuck
  *   O[t,i] = sum_n exp(S[t,i,n] - lse[t,i]) V row n
  * over the rows n up to t's own position (all kv_len rows if the context is not causal).  With shared_kv the key is the latent
  * row rotated to n and the value the row itself.  A token that sees no row has O = 0 and lse = -infinity.  What rows that a token
- * does not see hold (Inf and NaN included) does not reach it.
+ * does not see hold (Inf and NaN included) does not reach it; NaN in its query or in keys that it sees makes its O and lse NaN.
+ * Sums, maxima and lse are fp32.  In bf16 a rotated shared key is two bf16 parts, and a probability is two for sequences of up to
+ * 32 (token, head) rows, 64 with r3, rt3 <= 64 -- one where the batch may have more rows in any sequence (max_new * n_heads), or
+ * max_len is above 512 and the batch has more sequences than half the compute units (with a rotated shared latent wider than 64
+ * than all of them), or a prefix: O then has the error of one more rounding (relative L2 0.0023 in place of 0.0017), lse the same.
  *   Q    device [T, n_heads, r3]   in: per-head queries, rotated (Qrot of tucker_attn_append_paged)
  *   O    device [T, n_heads, rt3]  out, storage type
  *   lse  device [T, n_heads] fp32  out, natural logarithm; may be NULL
@@ -343,8 +349,8 @@ int tucker_attn_attend_prefix(tucker_attn_ctx *ctx, const tucker_attn_pages *pag
  *   X   device [T, d_model]   in: the tokens of all sequences, one sequence behind the other (q_start)
  *   Y   device [T, d_model]   out, storage type; rows of X behind the last sequence leave rows of Y that mean nothing
  * Serves prompts, pieces of prompts, proposed and single tokens, any mixture of them in one step.  prefix_table may be NULL with
- * prefix_len 0; the prefix's rows are appended beforehand, by a call without one.  Differs from forward and decode in that the
- * per-head queries and outputs pass through memory in the storage type (bf16: two more roundings).
+ * prefix_len 0; the prefix's rows are appended beforehand, by a call without one.  Differs from forward and decode in that
+ * keys and per-head queries pass through memory in the storage type before they are rotated (bf16: one more rounding of each).
  *   workspace  device, >= tucker_attn_forward_paged_workspace_bytes bytes, 256-byte aligned; scratch
  * Limits and refusals: those of append and attend above, and 65535 * 32 tokens.
  */

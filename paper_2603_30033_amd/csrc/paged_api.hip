@@ -74,7 +74,9 @@ int part_keys(int keys, int& parts) {
   return each;
 }
 
-// Longest keys that one workgroup takes alone rather than several and a second launch that joins their results
+// Longest keys that one workgroup takes alone rather than several and a second launch that joins their results.  us with 256, 512, 1024, 32
+// heads of 128 channels: one sequence of 300 rows 15.8, 12.4, 12.5; of 500 15.5, 14.4, 14.4; of 700 15.4, 15.4, 18.3; of 1000 15.4, 15.5,
+// 22.1; 64 of 1000 19.2, 19.0, 23.4.
 constexpr int kStreamWhole = 512;
 
 // What of a call depends on its bounds alone: which kernels, the parts of their work, the workspace.  Returns its bytes.
@@ -85,6 +87,8 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const int keys = b->max_len - prefix;
   const bool tile = f.dtype == TUCKER_ATTN_BF16;                  // (fp32 rows go through paged_rows)
   const int block = tile ? kTileRows : 32;
+  // least keys of a prefix's part, us with half, these, twice: seven sequences behind 777 rows, 12 heads of 64, 12.3, 12.9, 15.2 (fp32 19.3,
+  // 19.6, 22.9); four behind 2000, 32 heads of 128, 14.1, 16.6, 22.5; two behind 16384 15.5, 16.4, 21.3; 32 behind 16384 30.7, 30.8, 30.9
   a.prefix_parts = prefix > 0 ? key_parts(c, (rows + block - 1) / block, prefix, tile ? 1 : 2, tile ? 256 : 128) : 0;
   if (tile && prefix > 0) {
     // ... and no more of the two workgroups a compute unit than its share of the work, the sequences' own keys at half their bound (128
@@ -97,10 +101,14 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
   const long pieces = (rows + block - 1) / block * a.prefix_parts;
   a.prefix_wgs = (int)((pieces + 7) / 8 * 8);
   // Few rows and no prefix: paged_stream, unless there are so many sequences that its workgroups could not have equal shares.  us,
-  // 32 heads of 128 channels, paged_stream and paged_tile: 128 sequences of up to 1024 rows 22, 24; 140: 32, 25; 200: 37, 27; 16 of 4096
-  // 21, 22; one of 32768 19, 21; 12 heads of 64: 1 of 257 8, 12; 140 of 3000 28, 24; a shared latent: 140 of 3000 37, 42, 250 68, 55.
-  // Behind a prefix their keys go with the prefix's own launch, which paged_tile does (two launches of these kernels: 32 sequences
-  // behind 16384 rows 44 and 35; 128 with up to 1024 rows of their own 46 and 33; 16 with 32768 68 and 57).
+  // 32 heads of 128 channels, paged_stream and paged_tile: 128 sequences of up to 1024 rows 20.4, 23.1; 140: 25.2, 23.3; 200: 28.2, 25.4;
+  // 16 of 4096 19.2, 21.4; one of 32768 17.9, 19.9; 12 heads of 64: one of 257 8.4, 11.2; 140 of up to 3000 30.6, 21.9, of 3000 42.2, 28.7; a
+  // shared latent (twice the workgroups): 140 of 3000 55.4, 57.6, 250 72.1, 102.7.
+  // One more row than paged_stream takes: 16 sequences of 4096 with 32 heads 18.1, with 33 23.2, with 64 27.1, with 2 tokens of 32 27.9.
+  // A prompt's piece sends the single tokens beside it to paged_tile: 32 of them on 2000 rows 18.4, 512 tokens on 2048 46.8, in one call 50.3.
+  // Behind a prefix their keys go with the prefix's own launch, which paged_tile does (with this kernel beside it, in two launches, before
+  // the joins became what they are: 32 sequences behind 16384 rows 44, in one 35; 128 with up to 1024 rows of their own 46, 33; 16 with
+  // 32768 68, 57).
   const int wgs = (stream_late(c->D, f.shared_kv && f.use_rope ? 1 : 0) ? 2 : 1) * c->n_cus;
   const bool split = keys > kStreamWhole;
   const bool even = 2 * (long)b->B <= wgs && b->B <= 256 && (long)b->B * (keys / kStreamUnit + 1) < (1l << 31);   // (units in 32 bits)
@@ -123,6 +131,8 @@ size_t plan(const tucker_attn_ctx* c, const tucker_attn_batch* b, int prefix, vo
     a.tile_per_key = 1. / (kTileUnit * (double)f.n_heads);
     shared = 2l * a.tile_wgs * kTileRows;
   } else {
+    // (least keys 64, 128, 256: five proposed tokens on 700 rows, three sequences of 12 heads of 64, 12.6, 12.9, 16.2 us; one token on 257
+    // 11.8, 11.8, 14.8)
     int parts = key_parts(c, paged_rows_blocks(a, block), keys, 2, 128);
     a.own_keys = part_keys(keys, parts);
     if (parts > 1) a.own_parts = parts;
