@@ -312,8 +312,9 @@ size_t tucker_attn_attend_workspace_bytes(const tucker_attn_ctx *ctx, const tuck
  *   S[t,i,n] = <Q[t,i], K row n of t's sequence> / sqrt(d_head),  lse[t,i] = log sum_n exp S[t,i,n],
  *   O[t,i] = sum_n exp(S[t,i,n] - lse[t,i]) V row n
  * over the rows n up to t's own position (all kv_len rows if the context is not causal).  With shared_kv the key is the latent
- * row rotated to n and the value the row itself.  A token that sees no row has O = 0 and lse = -infinity.  What rows that a token
- * does not see hold (Inf and NaN included) does not reach it; NaN in its query or in keys that it sees makes its O and lse NaN.
+ * row rotated to n and the value the row itself.  A token that sees no row, or (its values being finite) none with a score above
+ * -infinity, has O = 0 and lse = -infinity.  What rows that a token does not see hold (Inf and NaN included) does not reach it; NaN
+ * in its query or in keys that it sees makes its O and lse NaN.
  * Sums, maxima and lse are fp32.  In bf16 a rotated shared key is two bf16 parts, and a probability is two for sequences of up to
  * 32 (token, head) rows, 64 with r3, rt3 <= 64 -- one where the batch may have more rows in any sequence (max_new * n_heads), or
  * max_len is above 512 and the batch has more sequences than half the compute units (with a rotated shared latent wider than 64

@@ -47,13 +47,11 @@ def test_a_query_that_is_nan(call, dtype, heads, r, shared):
 
 
 @pytest.mark.parametrize("dtype,heads,r", LAYERS)
-@pytest.mark.parametrize("where", ["last", "later half", "prefix", "own"])
-@pytest.mark.parametrize("call", ["long", "pieces", "many", "prefix"])
+@pytest.mark.parametrize("call,where", [(c, w) for c in ("long", "pieces", "many", "prefix") for w in ("last", "later half", "prefix", "own")
+                                        if w != "prefix" or c == "prefix"])
 def test_keys_that_are_nan(call, where, dtype, heads, r):
     new, rows, prefix = CALLS[call]
     b = Batch(new, rows, 16, r, r, heads, DT[dtype], prefix=prefix, seed=32, fill=0.0)
-    if where == "prefix" and not prefix:
-        pytest.skip("no prefix")
     O, L = run(b, heads, r, dtype)
     at = b.rows_of(0)
     lo, hi = {"last": (rows[0] - 1, rows[0]), "later half": (rows[0] // 2, rows[0]), "prefix": (0, prefix), "own": (prefix, rows[0])}[where]
@@ -117,3 +115,18 @@ def test_an_infinite_channel_of_a_shared_latent(call, dtype, heads, r, sign):
         tol = size * ((2.0 ** -16 if dtype == "bf16" else 0) + (r + 2) * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -21 + (len(keep) + 64) * 2.0 ** -24
         assert ((L[t].cpu().double() - lse).abs() <= tol + lse.abs() * 2.0 ** -22).all()
     assert torch.isinf(with_zero[0])
+
+
+@pytest.mark.parametrize("dtype,heads,r", LAYERS)
+@pytest.mark.parametrize("new,rows,prefix", [([1, 1, 1], [1, 4097, 70], 0), ([40, 1, 3], [40, 1500, 70], 0), ([1, 1, 1], [701, 1900, 750], 700)])
+def test_keys_without_any_weight(new, rows, prefix, dtype, heads, r):
+    # all scores -infinity: as if the tokens saw no row
+    b = Batch(new, rows, 16, r, r, heads, DT[dtype], prefix=prefix, seed=34, fill=0.0)
+    b.Q[..., 0] = -(b.Q[..., 0].float().abs() + 0.5).to(DT[dtype])
+    others = run(b, heads, r, dtype)
+    for s in range(3 if prefix else 2):
+        b.K.view(-1, r)[b.rows_of(s), 0] = math.inf
+    O, L = run(b, heads, r, dtype)
+    n = int(b.q_start[3 if prefix else 2])
+    assert (O[:n] == 0).all() and (L[:n] == -math.inf).all()
+    assert torch.equal(O[n:], others[0][n:]) and torch.equal(L[n:], others[1][n:])
